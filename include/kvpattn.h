@@ -20,7 +20,8 @@
  *     keeps no reference to them after it returns.
  *   - `stream` is a hipStream_t (NULL = the legacy default stream).  Every call is asynchronous on it.
  *     A stream under graph capture is refused (KVP_EHIP, nothing is enqueued) by the calls that read host arrays:
- *     a graph would outlive their copies.  paged_decode_attn_noalloc can be captured.
+ *     a graph would outlive their copies.  paged_decode_attn_noalloc, kvp_rope_apply and linear_decode_attn can be
+ *     captured.
  *   - Page ids read from device block tables are range-checked on the device.  An id outside
  *     [0, num_pages) is never dereferenced: the kernels skip that page and record KVP_ERANGE in the
  *     pool's device error word, which kv_pool_device_error() returns.  Such device-side errors are
@@ -250,6 +251,102 @@ int mixed_step_attn(kvp_pool_t pool, int layer, int num_q_heads, float scale, in
                     const kvp_group_prefix* group_prefix, void* out_dec, const void* q_pf,
                     const int32_t* block_tables_pf, int maxp_pf, const int32_t* ctx_lens, const int32_t* cu_q,
                     int num_pf, void* out_pf, void* ws, size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------------------
+ * Rotary positions — queries and keys are turned by their position before attention
+ * ------------------------------------------------------------------------------------------------- */
+
+/* A rotation: plain host memory of the caller, filled by kvp_rope_init, read during the calls it is passed to.
+ * turns[i] = 2^64 * f_i / (2 pi) modulo 2^64, f_i the angle of pair i per position in radians. */
+#define KVP_ROPE_PAIRS 128
+typedef struct kvp_rope {
+  int32_t rotary_dim, interleaved;
+  float magnitude;
+  int32_t valid; /* set by kvp_rope_init */
+  uint64_t turns[KVP_ROPE_PAIRS];
+} kvp_rope;
+
+/* Fill *rope for the first rotary_dim dims of a head (even, 2..256); the others are not rotated.
+ *   interleaved   0: pair i is dims (i, i + rotary_dim / 2);  1: dims (2 i, 2 i + 1)
+ *   base          f_i = base^(-2 i / rotary_dim)  (>= 1)
+ *   factor        >= 1: contexts are factor times longer than the original ones (1: as they are)
+ *   original_len  0: every f_i is divided by factor.  > 0: with n_i = original_len f_i / (2 pi) turns over the original
+ *                 context and g_i = (n_i - low_turns) / (high_turns - low_turns) clamped to [0, 1],
+ *                 f_i becomes (1 - g_i) f_i / factor + g_i f_i  (0 <= low_turns < high_turns)
+ *   magnitude     the rotated dims are multiplied by it (1: none; finite, > 0)
+ * Pure host computation.  Errors: KVP_EINVAL for a value outside these ranges. */
+int kvp_rope_init(kvp_rope* rope, int rotary_dim, int interleaved, double base, double factor, int original_len,
+                  double low_turns, double high_turns, double magnitude);
+
+/* y = the heads of x turned by their token's position: for each pair (a, b), with angle = position f_i,
+ *   y_a = magnitude (x_a cos(angle) - x_b sin(angle)),  y_b = magnitude (x_a sin(angle) + x_b cos(angle)).
+ * grad != 0: the transpose, angle -> -angle, which takes the gradient of y to the gradient of x.
+ *   x, y       device, KVP_BF16 or KVP_F32 (both the same): head h of token t is the head_dim elements from
+ *              t * token_stride + h * head_stride.  y may be x with the same strides, or must not overlap it; y's
+ *              heads must not overlap each other.
+ *   positions  device int32 [num_tokens], any values
+ *   head_dim   rotary_dim..256
+ * Computed in fp32 (the angle modulo a turn in 64-bit integers) and rounded once.  Reads no host memory after it
+ * returns, so it can be captured. */
+int kvp_rope_apply(const kvp_rope* rope, const void* x, int64_t x_token_stride, int64_t x_head_stride, void* y,
+                   int64_t y_token_stride, int64_t y_head_stride, int dtype, const int32_t* positions,
+                   int64_t num_tokens, int num_heads, int head_dim, int grad, void* stream);
+
+/* kv_append of keys that are turned on the way: the key of the token at logical position p is stored as kvp_rope_apply
+ * gives it at position p (in an FP8 pool rounded once, from fp32 to E4M3), the value as kv_append stores it.  With
+ * q, the same tokens' queries are turned in the same launch and written to q_out.
+ *   k, v    device bf16: token t's num_kv_heads * head_dim elements from t * k_stride, t * v_stride (rows of a fused
+ *           projection, for instance)
+ *   q       device bf16, nullable (then q_out and num_q_heads are ignored): token t's num_q_heads * head_dim elements
+ *           from t * q_stride.  q_out likewise; it may be q with the same stride, or must not overlap it.
+ * Strides are in elements, multiples of 8, and the pointers 16-byte aligned; q_out_stride is at least
+ * num_q_heads * head_dim.  rotary_dim is at most head_dim.  The pool must live on the current device.  Everything else
+ * as in kv_append; a token whose page id is outside the pool is skipped, its query is turned all the same. */
+int kv_append_rope(kvp_pool_t pool, int layer, const kvp_rope* rope, const void* k, int64_t k_stride, const void* v,
+                   int64_t v_stride, const void* q, int64_t q_stride, void* q_out, int64_t q_out_stride,
+                   int num_q_heads, const int32_t* block_tables, int maxp, const int32_t* start_pos,
+                   const int32_t* cu_new, int num_seqs, const kvp_group_prefix* gp, void* stream);
+
+/* ---------------------------------------------------------------------------------------------------
+ * Linear attention with a decay per head — layers whose sessions keep a state instead of pages
+ *
+ *   S_t = decay[h] S_{t-1} + k_t v_t^T,   o_t = scale * q_t^T S_t     (per KV head h; S is [head_dim, head_dim])
+ *
+ * The states are the caller's: device fp32 [num_slots][num_kv_heads][head_dim (of k)][head_dim (of v)].  Sequence i
+ * continues from slot src_slots[i] (-1: from zeros) and leaves its state in slot dst_slots[i] (-1: it is not kept).
+ * The samples of a rollout group fork from their prompt's state by naming its slot as their source.  A destination
+ * may be its own sequence's source; it must not be another's source or destination.
+ *
+ * Common arguments:
+ *   q           device bf16, token t's num_q_heads * head_dim elements from t * q_stride; query head h reads KV head
+ *               h / (num_q_heads / num_kv_heads)
+ *   k, v        device bf16, token t's num_kv_heads * head_dim elements from t * k_stride, t * v_stride
+ *   decay       host float [num_kv_heads], each in (0, 1]
+ *   src_slots, dst_slots   host int32 [num_seqs]
+ *   scale       finite
+ *   out         device [tokens, num_q_heads, head_dim], out_dtype KVP_BF16 or KVP_F32
+ * Strides are in elements, multiples of 8, and the pointers 16-byte aligned.  head_dim is 64 or 128, num_kv_heads at
+ * most KVP_LINEAR_MAX_HEADS.  An infinity or NaN in a token's q, k or v leaves earlier tokens, other heads and other
+ * sequences as they are.
+ * Errors: KVP_ERANGE for a slot outside [-1, num_slots); KVP_EINVAL for a destination that is another sequence's
+ * source or destination, or a decay outside (0, 1]; KVP_EUNSUPPORTED for heads or dtypes not named here.
+ * ------------------------------------------------------------------------------------------------- */
+#define KVP_LINEAR_MAX_HEADS 128
+
+/* Chunks: sequence i's tokens are the rows cu[i] .. cu[i+1] (none: its state is handed on as it is).
+ *   cu  host int32 [num_seqs + 1], non-decreasing, cu[0] = 0 */
+int linear_chunk_workspace_size(const int32_t* cu, int num_seqs, int num_kv_heads, int head_dim, size_t* bytes);
+int linear_chunk_attn(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                      float* state, int num_slots, const float* decay, const int32_t* src_slots,
+                      const int32_t* dst_slots, const int32_t* cu, int num_seqs, int num_q_heads, int num_kv_heads,
+                      int head_dim, float scale, void* out, int out_dtype, void* ws, size_t ws_bytes, void* stream);
+
+/* One token per sequence: row i of q, k, v and out.  Reads no host memory after it returns, so it can be captured (the
+ * graph keeps the slots and decays of the capture). */
+int linear_decode_attn(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                       int64_t v_stride, float* state, int num_slots, const float* decay, const int32_t* src_slots,
+                       const int32_t* dst_slots, int num_seqs, int num_q_heads, int num_kv_heads, int head_dim,
+                       float scale, void* out, int out_dtype, void* stream);
 
 /* ---------------------------------------------------------------------------------------------------
  * CPU KV tier (Sec. 5.5: a host-memory tier keeps a backup copy of GPU-resident KV, so the GPU pool can

@@ -21,7 +21,7 @@ LIB_NAME = "libkvpattn.so"
 LIB_PATH = os.path.join(HERE, LIB_NAME)
 
 SOURCES = ["plan.cpp", "api.cpp", "append.hip", "decode.hip", "prefill.hip", "prefill_long.hip", "mixed.hip",
-           "tier.hip", "prefix.hip"]
+           "tier.hip", "prefix.hip", "rope.hip", "linear.hip"]
 ARCH = "gfx950"
 COMMON = ["-O3", "-fPIC", "-std=c++17", "-Wall", "-Wno-unused-result", f"-I{os.path.join(ROOT, 'include')}"]
 HIP_ONLY = [f"--offload-arch={ARCH}", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

@@ -9,8 +9,10 @@
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
+#include <exception>
 #include <mutex>
 #include <string>
+#include <utility>
 #include <vector>
 
 #include "kvp_kernels.h"
@@ -553,6 +555,161 @@ int layout_mixed(kvp_pool_t pool, int num_q_heads, const int32_t* seq_lens, int 
   return KVP_OK;
 }
 
+// The checks and page runs of kv_append and kv_append_rope (nothing is enqueued).
+int plan_append(const void* k, const void* v, const int32_t* block_tables, int maxp, const int32_t* start_pos,
+                const int32_t* cu_new, int num_seqs, const kvp_group_prefix* gp, std::vector<kvp::PageRun>* runs) {
+  if (!start_pos || !cu_new || !block_tables) return set_err(KVP_EINVAL, "NULL metadata pointer");
+  if (cu_new[0] != 0) return set_err(KVP_EINVAL, "cu_new[0] = %d, must be 0", cu_new[0]);
+  std::vector<int32_t> cnt(num_seqs);
+  std::vector<int64_t> first(num_seqs);
+  for (int i = 0; i < num_seqs; ++i) {
+    cnt[i] = cu_new[i + 1] - cu_new[i];
+    first[i] = cu_new[i];
+    if (cnt[i] < 0) return set_err(KVP_EINVAL, "cu_new decreases at %d", i);
+    if (start_pos[i] < 0) return set_err(KVP_EINVAL, "start_pos[%d] = %d < 0", i, start_pos[i]);
+    if ((int64_t)start_pos[i] + cnt[i] > (int64_t)maxp * kvp::kPage)
+      return set_err(KVP_ERANGE, "sequence %d: positions up to %lld exceed maxp * 16 = %lld", i,
+                     (long long)start_pos[i] + cnt[i], (long long)maxp * kvp::kPage);
+  }
+  if (cu_new[num_seqs] > 0 && (!k || !v)) return set_err(KVP_EINVAL, "k or v is NULL");
+  if (gp) {
+    kvp::Status st = kvp::validate_group_prefix(nullptr, num_seqs, gp);
+    if (!st.ok()) return from_status(st);
+    if (gp->num_groups > 0)
+      for (int i = 0; i < num_seqs; ++i) {
+        const int g = gp->group_id[i];
+        if (g >= 0 && cnt[i] > 0 && (int64_t)start_pos[i] < (int64_t)gp->shared_pages[g] * kvp::kPage)
+          return set_err(KVP_ESHARED, "sequence %d would write position %d inside its group's %d shared pages", i,
+                         start_pos[i], gp->shared_pages[g]);
+      }
+  }
+  build_runs(start_pos, first.data(), cnt.data(), num_seqs, runs);
+  return KVP_OK;
+}
+
+kvp::AppendArgs append_args(kvp_pool_t pool, int layer, const void* k, const void* v, const int32_t* block_tables,
+                            int maxp, const Staging::Lease& lease, size_t n_runs) {
+  kvp::AppendArgs a{};
+  a.k = reinterpret_cast<const uint16_t*>(k);
+  a.v = reinterpret_cast<const uint16_t*>(v);
+  a.layer = const_cast<uint16_t*>(layer_ptr(pool, layer));
+  a.bt = block_tables;
+  a.runs = reinterpret_cast<const kvp::PageRun*>(lease.host);
+  a.n_runs = (int)n_runs;
+  a.maxp = maxp;
+  a.Hkv = pool->num_kv_heads;
+  a.num_pages = pool->num_pages;
+  a.err = pool->err;
+  a.fp8 = pool->dtype == KVP_FP8_E4M3;
+  a.inv_scale_k = 1.0f / pool->k_scale[layer];
+  a.inv_scale_v = 1.0f / pool->v_scale[layer];
+  return a;
+}
+
+int check_cu(const int32_t* cu, int num_seqs) {
+  if (!cu) return set_err(KVP_EINVAL, "cu is NULL");
+  if (cu[0] != 0) return set_err(KVP_EINVAL, "cu[0] = %d, must be 0", cu[0]);
+  for (int i = 0; i < num_seqs; ++i)
+    if (cu[i + 1] < cu[i]) return set_err(KVP_EINVAL, "cu decreases at %d", i);
+  return KVP_OK;
+}
+
+constexpr int32_t kRopeValid = 0x726f7065;  // kvp_rope.valid
+
+// Rows of bf16 that a kernel reads or writes 16 bytes at a time.
+int check_rows(const void* p, int64_t stride, const char* name) {
+  if (!p) return set_err(KVP_EINVAL, "%s is NULL", name);
+  if ((reinterpret_cast<uintptr_t>(p) & 15) != 0) return set_err(KVP_EINVAL, "%s is not 16-byte aligned", name);
+  if (stride < 0 || stride % 8 != 0)
+    return set_err(KVP_EINVAL, "%s stride %lld is not a multiple of 8 elements", name, (long long)stride);
+  return KVP_OK;
+}
+
+int check_rope(const kvp_rope* rope, int head_dim) {
+  if (!rope || rope->valid != kRopeValid) return set_err(KVP_EINVAL, "rope is NULL or not initialised");
+  if (rope->rotary_dim > head_dim)
+    return set_err(KVP_EINVAL, "rotary_dim %d exceeds head_dim %d", rope->rotary_dim, head_dim);
+  return KVP_OK;
+}
+
+kvp::RopeTable rope_table(const kvp_rope& rope) {
+  kvp::RopeTable t;
+  std::memcpy(t.turns, rope.turns, sizeof(t.turns));
+  t.rotary_dim = rope.rotary_dim;
+  t.interleaved = rope.interleaved;
+  t.magnitude = rope.magnitude;
+  return t;
+}
+
+// Checks of the linear attention calls (before anything is enqueued).
+int check_linear(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                 const float* state, int num_slots, const float* decay, const int32_t* src, const int32_t* dst,
+                 int num_seqs, bool rows, int num_q_heads, int num_kv_heads, int head_dim, float scale, const void* out,
+                 int out_dtype) {
+  if (head_dim != 64 && head_dim != 128) return set_err(KVP_EUNSUPPORTED, "head_dim %d (64 or 128)", head_dim);
+  if (num_kv_heads <= 0 || num_kv_heads > KVP_LINEAR_MAX_HEADS)
+    return set_err(KVP_EUNSUPPORTED, "num_kv_heads %d outside [1, %d]", num_kv_heads, KVP_LINEAR_MAX_HEADS);
+  const int G = num_q_heads / num_kv_heads;
+  if (num_q_heads <= 0 || num_q_heads % num_kv_heads || G > 16 || (G & (G - 1)))
+    return set_err(KVP_EUNSUPPORTED, "num_q_heads / num_kv_heads = %d / %d is not 1, 2, 4, 8 or 16", num_q_heads,
+                   num_kv_heads);
+  if (out_dtype != KVP_BF16 && out_dtype != KVP_F32) return set_err(KVP_EUNSUPPORTED, "out_dtype %d", out_dtype);
+  if (!std::isfinite(scale)) return set_err(KVP_EINVAL, "scale must be finite");
+  if (!state || num_slots <= 0) return set_err(KVP_EINVAL, "state is NULL or without slots");
+  if ((reinterpret_cast<uintptr_t>(state) & 15) != 0) return set_err(KVP_EINVAL, "state is not 16-byte aligned");
+  if (!decay || !src || !dst) return set_err(KVP_EINVAL, "decay, src_slots or dst_slots is NULL");
+  if (rows) {
+    int rc = check_rows(q, q_stride, "q");
+    if (!rc) rc = check_rows(k, k_stride, "k");
+    if (!rc) rc = check_rows(v, v_stride, "v");
+    if (!rc) rc = check_rows(out, 0, "out");
+    if (rc) return rc;
+  }
+  for (int h = 0; h < num_kv_heads; ++h)
+    if (!(decay[h] > 0.0f && decay[h] <= 1.0f))
+      return set_err(KVP_EINVAL, "decay[%d] = %g is not in (0, 1]", h, (double)decay[h]);
+  for (int i = 0; i < num_seqs; ++i)
+    if (src[i] < -1 || src[i] >= num_slots || dst[i] < -1 || dst[i] >= num_slots)
+      return set_err(KVP_ERANGE, "sequence %d: slots %d -> %d outside [-1, %d)", i, src[i], dst[i], num_slots);
+  // A destination has one writer, and no reader but its writer: (slot, sequence) sorted by slot.
+  std::vector<std::pair<int32_t, int32_t>> writes;
+  writes.reserve(num_seqs);
+  for (int i = 0; i < num_seqs; ++i)
+    if (dst[i] >= 0) writes.emplace_back(dst[i], i);
+  std::sort(writes.begin(), writes.end());
+  for (size_t j = 1; j < writes.size(); ++j)
+    if (writes[j].first == writes[j - 1].first)
+      return set_err(KVP_EINVAL, "slot %d is the destination of sequences %d and %d", writes[j].first,
+                     writes[j - 1].second, writes[j].second);
+  for (int i = 0; i < num_seqs; ++i) {
+    if (src[i] < 0 || src[i] == dst[i]) continue;
+    const auto w = std::lower_bound(writes.begin(), writes.end(), std::make_pair(src[i], (int32_t)0));
+    if (w != writes.end() && w->first == src[i])
+      return set_err(KVP_EINVAL, "slot %d is the source of sequence %d and the destination of sequence %d", src[i], i,
+                     w->second);
+  }
+  return KVP_OK;
+}
+
+kvp::LinearArgs linear_args(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                            int64_t v_stride, float* state, int num_q_heads, int num_kv_heads, float scale, void* out,
+                            int out_dtype) {
+  kvp::LinearArgs a{};
+  a.q = reinterpret_cast<const uint16_t*>(q);
+  a.k = reinterpret_cast<const uint16_t*>(k);
+  a.v = reinterpret_cast<const uint16_t*>(v);
+  a.q_stride = q_stride;
+  a.k_stride = k_stride;
+  a.v_stride = v_stride;
+  a.state = state;
+  a.out = out;
+  a.out_f32 = out_dtype == KVP_F32;
+  a.Hq = num_q_heads;
+  a.Hkv = num_kv_heads;
+  a.scale = scale;
+  return a;
+}
+
 }  // namespace
 
 extern "C" {
@@ -687,56 +844,210 @@ int kv_append(kvp_pool_t pool, int layer, const void* k, const void* v, const in
   if (rc) return rc;
   if (num_seqs < 0 || maxp < 0) return set_err(KVP_EINVAL, "num_seqs %d / maxp %d negative", num_seqs, maxp);
   if (num_seqs == 0) return KVP_OK;
-  if (!start_pos || !cu_new || !block_tables) return set_err(KVP_EINVAL, "NULL metadata pointer");
-  if (cu_new[0] != 0) return set_err(KVP_EINVAL, "cu_new[0] = %d, must be 0", cu_new[0]);
-  std::vector<int32_t> cnt(num_seqs);
-  std::vector<int64_t> first(num_seqs);
-  for (int i = 0; i < num_seqs; ++i) {
-    cnt[i] = cu_new[i + 1] - cu_new[i];
-    first[i] = cu_new[i];
-    if (cnt[i] < 0) return set_err(KVP_EINVAL, "cu_new decreases at %d", i);
-    if (start_pos[i] < 0) return set_err(KVP_EINVAL, "start_pos[%d] = %d < 0", i, start_pos[i]);
-    if ((int64_t)start_pos[i] + cnt[i] > (int64_t)maxp * kvp::kPage)
-      return set_err(KVP_ERANGE, "sequence %d: positions up to %lld exceed maxp * 16 = %lld", i,
-                     (long long)start_pos[i] + cnt[i], (long long)maxp * kvp::kPage);
-  }
-  if (cu_new[num_seqs] > 0 && (!k || !v)) return set_err(KVP_EINVAL, "k or v is NULL");
-  if (gp) {
-    kvp::Status st = kvp::validate_group_prefix(nullptr, num_seqs, gp);
-    if (!st.ok()) return from_status(st);
-    if (gp->num_groups > 0)
-      for (int i = 0; i < num_seqs; ++i) {
-        const int g = gp->group_id[i];
-        if (g >= 0 && cnt[i] > 0 && (int64_t)start_pos[i] < (int64_t)gp->shared_pages[g] * kvp::kPage)
-          return set_err(KVP_ESHARED, "sequence %d would write position %d inside its group's %d shared pages", i,
-                         start_pos[i], gp->shared_pages[g]);
-      }
-  }
   std::vector<kvp::PageRun> runs;
-  build_runs(start_pos, first.data(), cnt.data(), num_seqs, &runs);
+  rc = plan_append(k, v, block_tables, maxp, start_pos, cu_new, num_seqs, gp, &runs);
+  if (rc) return rc;
   if (runs.empty()) return KVP_OK;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   Staging::Lease lease;
   rc = lease_runs(runs, s, &lease);
   if (rc) return rc;
-  kvp::AppendArgs a{};
-  a.k = reinterpret_cast<const uint16_t*>(k);
-  a.v = reinterpret_cast<const uint16_t*>(v);
-  a.layer = const_cast<uint16_t*>(layer_ptr(pool, layer));
-  a.bt = block_tables;
-  a.runs = reinterpret_cast<const kvp::PageRun*>(lease.host);
-  a.n_runs = (int)runs.size();
-  a.maxp = maxp;
-  a.Hkv = pool->num_kv_heads;
-  a.num_pages = pool->num_pages;
-  a.err = pool->err;
-  a.fp8 = pool->dtype == KVP_FP8_E4M3;
-  a.inv_scale_k = 1.0f / pool->k_scale[layer];
-  a.inv_scale_v = 1.0f / pool->v_scale[layer];
-  hipError_t e = kvp::launch_append(a, pool->head_dim, s);
+  hipError_t e = kvp::launch_append(append_args(pool, layer, k, v, block_tables, maxp, lease, runs.size()),
+                                    pool->head_dim, s);
   const int rr = staging().release(lease, e == hipSuccess);
   if (e != hipSuccess) return hip_err(e, "kv_append launch");
   return rr;
+}
+
+int kv_append_rope(kvp_pool_t pool, int layer, const kvp_rope* rope, const void* k, int64_t k_stride, const void* v,
+                   int64_t v_stride, const void* q, int64_t q_stride, void* q_out, int64_t q_out_stride,
+                   int num_q_heads, const int32_t* block_tables, int maxp, const int32_t* start_pos,
+                   const int32_t* cu_new, int num_seqs, const kvp_group_prefix* gp, void* stream) try {
+  int rc = check_layer(pool, layer);
+  if (!rc) rc = check_rope(rope, pool->head_dim);
+  if (rc) return rc;
+  if (num_seqs < 0 || maxp < 0) return set_err(KVP_EINVAL, "num_seqs %d / maxp %d negative", num_seqs, maxp);
+  if (num_seqs == 0) return KVP_OK;
+  std::vector<kvp::PageRun> runs;
+  rc = plan_append(k, v, block_tables, maxp, start_pos, cu_new, num_seqs, gp, &runs);
+  if (rc) return rc;
+  if (runs.empty()) return KVP_OK;
+  rc = check_rows(k, k_stride, "k");
+  if (!rc) rc = check_rows(v, v_stride, "v");
+  if (!rc && q) {
+    rc = check_rows(q, q_stride, "q");
+    if (!rc) rc = check_rows(q_out, q_out_stride, "q_out");
+    if (!rc && (num_q_heads <= 0 || num_q_heads % pool->num_kv_heads))
+      rc = set_err(KVP_EUNSUPPORTED, "num_q_heads %d is not a multiple of the pool's %d KV heads", num_q_heads,
+                   pool->num_kv_heads);
+    if (!rc && q_out_stride < (int64_t)num_q_heads * pool->head_dim)
+      rc = set_err(KVP_EINVAL, "q_out stride %lld is less than a row of %d heads", (long long)q_out_stride, num_q_heads);
+    if (!rc && q_out == q && q_out_stride != q_stride)
+      rc = set_err(KVP_EINVAL, "q_out is q with another stride");
+  }
+  if (rc) return rc;
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return hip_err(e, "hipGetDevice");
+  if (dev != pool->device)
+    return set_err(KVP_EINVAL, "the pool lives on device %d, the current device is %d", pool->device, dev);
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  Staging::Lease lease;
+  rc = lease_runs(runs, s, &lease);
+  if (rc) return rc;
+  kvp::AppendRopeArgs a{};
+  a.kv = append_args(pool, layer, k, v, block_tables, maxp, lease, runs.size());
+  a.table = rope_table(*rope);
+  a.k_stride = k_stride;
+  a.v_stride = v_stride;
+  a.q = reinterpret_cast<const uint16_t*>(q);
+  a.q_out = reinterpret_cast<uint16_t*>(q_out);
+  a.q_stride = q_stride;
+  a.q_out_stride = q_out_stride;
+  a.Hq = q ? num_q_heads : 0;
+  e = kvp::launch_append_rope(a, pool->head_dim, s);
+  const int rr = staging().release(lease, e == hipSuccess);
+  if (e != hipSuccess) return hip_err(e, "kv_append_rope launch");
+  return rr;
+} catch (const std::exception& x) {
+  return set_err(KVP_ENOMEM, "kv_append_rope: %s", x.what());
+}
+
+int kvp_rope_init(kvp_rope* rope, int rotary_dim, int interleaved, double base, double factor, int original_len,
+                  double low_turns, double high_turns, double magnitude) {
+  if (!rope) return set_err(KVP_EINVAL, "rope is NULL");
+  if (rotary_dim < 2 || rotary_dim > 2 * KVP_ROPE_PAIRS || rotary_dim % 2)
+    return set_err(KVP_EINVAL, "rotary_dim %d is not even in [2, %d]", rotary_dim, 2 * KVP_ROPE_PAIRS);
+  if (!(base >= 1.0) || !std::isfinite(base)) return set_err(KVP_EINVAL, "base %g is not >= 1", base);
+  if (!(factor >= 1.0) || !std::isfinite(factor)) return set_err(KVP_EINVAL, "factor %g is not >= 1", factor);
+  if (original_len < 0) return set_err(KVP_EINVAL, "original_len %d < 0", original_len);
+  if (original_len > 0 && !(low_turns >= 0.0 && low_turns < high_turns && std::isfinite(high_turns)))
+    return set_err(KVP_EINVAL, "turns %g and %g are not 0 <= low < high", low_turns, high_turns);
+  if (!((float)magnitude > 0.0f) || !std::isfinite((float)magnitude))
+    return set_err(KVP_EINVAL, "magnitude %g is not finite and > 0", magnitude);
+  kvp_rope r{};
+  const long double two_pi = 6.283185307179586476925286766559L;
+  for (int i = 0; i < rotary_dim / 2; ++i) {
+    long double f = std::pow((long double)base, -2.0L * i / rotary_dim);
+    if (original_len == 0) {
+      f /= factor;
+    } else {
+      const long double n = original_len * f / two_pi;
+      const long double g = std::min(1.0L, std::max(0.0L, (n - low_turns) / ((long double)high_turns - low_turns)));
+      f = (1.0L - g) * f / factor + g * f;
+    }
+    r.turns[i] = (uint64_t)std::llrint(std::ldexp(f / two_pi, 64));  // f <= 1: at most 0.16 * 2^64
+  }
+  r.rotary_dim = rotary_dim;
+  r.interleaved = interleaved != 0;
+  r.magnitude = (float)magnitude;
+  r.valid = kRopeValid;
+  *rope = r;
+  return KVP_OK;
+}
+
+int kvp_rope_apply(const kvp_rope* rope, const void* x, int64_t x_token_stride, int64_t x_head_stride, void* y,
+                   int64_t y_token_stride, int64_t y_head_stride, int dtype, const int32_t* positions,
+                   int64_t num_tokens, int num_heads, int head_dim, int grad, void* stream) {
+  if (head_dim < 1 || head_dim > 256) return set_err(KVP_EUNSUPPORTED, "head_dim %d outside [1, 256]", head_dim);
+  int rc = check_rope(rope, head_dim);
+  if (rc) return rc;
+  if (dtype != KVP_BF16 && dtype != KVP_F32) return set_err(KVP_EUNSUPPORTED, "dtype %d (KVP_BF16 or KVP_F32)", dtype);
+  if (num_tokens < 0 || num_heads < 0)
+    return set_err(KVP_EINVAL, "num_tokens %lld or num_heads %d negative", (long long)num_tokens, num_heads);
+  if (num_tokens == 0 || num_heads == 0) return KVP_OK;
+  if (!x || !y || !positions) return set_err(KVP_EINVAL, "x, y or positions is NULL");
+  const uintptr_t es = dtype == KVP_F32 ? 4 : 2;
+  if (reinterpret_cast<uintptr_t>(x) % es || reinterpret_cast<uintptr_t>(y) % es)
+    return set_err(KVP_EINVAL, "x or y is not aligned to its elements");
+  if (num_tokens > INT64_MAX / 2 / ((int64_t)num_heads * 256))
+    return set_err(KVP_EINVAL, "num_tokens %lld is too large", (long long)num_tokens);
+  if (x_token_stride < 0 || x_head_stride < 0) return set_err(KVP_EINVAL, "negative x stride");
+  // y's heads are apart: inside a token, and from token to token (or the other way round)
+  const int64_t ts = y_token_stride, hs = y_head_stride;
+  const bool inner_heads = (num_heads == 1 || hs >= head_dim) && (num_tokens == 1 || ts >= (num_heads - 1) * hs + head_dim);
+  const bool inner_tokens = (num_tokens == 1 || ts >= head_dim) && (num_heads == 1 || hs >= (num_tokens - 1) * ts + head_dim);
+  if (ts < 0 || hs < 0 || !(inner_heads || inner_tokens)) return set_err(KVP_EINVAL, "y's heads overlap");
+  if (x == y && ((num_tokens > 1 && x_token_stride != ts) || (num_heads > 1 && x_head_stride != hs)))
+    return set_err(KVP_EINVAL, "y is x with other strides");
+  kvp::RopeArgs a{};
+  a.table = rope_table(*rope);
+  a.x = x;
+  a.y = y;
+  a.x_token = x_token_stride;
+  a.x_head = x_head_stride;
+  a.y_token = ts;
+  a.y_head = hs;
+  a.pos = positions;
+  a.tokens = num_tokens;
+  a.heads = num_heads;
+  a.D = head_dim;
+  a.grad = grad != 0;
+  const hipError_t e = kvp::launch_rope(a, dtype == KVP_F32, reinterpret_cast<hipStream_t>(stream));
+  return e == hipSuccess ? KVP_OK : hip_err(e, "kvp_rope_apply launch");
+}
+
+int linear_chunk_workspace_size(const int32_t* cu, int num_seqs, int num_kv_heads, int head_dim, size_t* bytes) {
+  if (!bytes) return set_err(KVP_EINVAL, "bytes is NULL");
+  *bytes = 0;
+  if (num_seqs < 0) return set_err(KVP_EINVAL, "num_seqs %d < 0", num_seqs);
+  return num_seqs == 0 ? KVP_OK : check_cu(cu, num_seqs);
+}
+
+int linear_chunk_attn(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                      float* state, int num_slots, const float* decay, const int32_t* src_slots,
+                      const int32_t* dst_slots, const int32_t* cu, int num_seqs, int num_q_heads, int num_kv_heads,
+                      int head_dim, float scale, void* out, int out_dtype, void* ws, size_t ws_bytes,
+                      void* stream) try {
+  if (num_seqs < 0) return set_err(KVP_EINVAL, "num_seqs %d < 0", num_seqs);
+  if (num_seqs == 0) return KVP_OK;
+  int rc = check_cu(cu, num_seqs);
+  if (!rc)
+    rc = check_linear(q, q_stride, k, k_stride, v, v_stride, state, num_slots, decay, src_slots, dst_slots, num_seqs,
+                      cu[num_seqs] > 0, num_q_heads, num_kv_heads, head_dim, scale, out, out_dtype);
+  if (rc) return rc;
+  std::vector<kvp::LinearItem> items;
+  for (int i = 0; i < num_seqs; ++i) items.push_back({cu[i], cu[i + 1] - cu[i], src_slots[i], dst_slots[i]});
+  const kvp::LinearArgs a = linear_args(q, q_stride, k, k_stride, v, v_stride, state, num_q_heads, num_kv_heads, scale,
+                                        out, out_dtype);
+  hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+  const size_t nb = items.size() * sizeof(kvp::LinearItem);
+  Staging::Lease lease;
+  rc = staging().lease(nb + num_kv_heads * sizeof(float), s, &lease);
+  if (rc) return rc;
+  unsigned char* host = reinterpret_cast<unsigned char*>(lease.host);
+  std::memcpy(host, items.data(), nb);
+  std::memcpy(host + nb, decay, num_kv_heads * sizeof(float));
+  const kvp::LinearItems list{reinterpret_cast<const kvp::LinearItem*>(host), reinterpret_cast<const float*>(host + nb)};
+  const hipError_t e = kvp::launch_linear_chunk(a, list, (int)items.size(), head_dim, s);
+  const int rr = staging().release(lease, e == hipSuccess);
+  return e == hipSuccess ? rr : hip_err(e, "linear_chunk_attn launch");
+} catch (const std::exception& x) {
+  return set_err(KVP_ENOMEM, "linear_chunk_attn: %s", x.what());
+}
+
+int linear_decode_attn(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                       int64_t v_stride, float* state, int num_slots, const float* decay, const int32_t* src_slots,
+                       const int32_t* dst_slots, int num_seqs, int num_q_heads, int num_kv_heads, int head_dim,
+                       float scale, void* out, int out_dtype, void* stream) try {
+  if (num_seqs < 0) return set_err(KVP_EINVAL, "num_seqs %d < 0", num_seqs);
+  if (num_seqs == 0) return KVP_OK;
+  const int rc = check_linear(q, q_stride, k, k_stride, v, v_stride, state, num_slots, decay, src_slots, dst_slots,
+                              num_seqs, true, num_q_heads, num_kv_heads, head_dim, scale, out, out_dtype);
+  if (rc) return rc;
+  const kvp::LinearArgs a = linear_args(q, q_stride, k, k_stride, v, v_stride, state, num_q_heads, num_kv_heads, scale,
+                                        out, out_dtype);
+  kvp::LinearList list{};
+  std::memcpy(list.decay, decay, sizeof(float) * num_kv_heads);
+  hipError_t e = hipSuccess;
+  for (int i = 0; i < num_seqs && e == hipSuccess; i += kvp::kLinearBatch) {
+    const int n = std::min(kvp::kLinearBatch, num_seqs - i);
+    for (int j = 0; j < n; ++j) list.items[j] = {i + j, 1, src_slots[i + j], dst_slots[i + j]};
+    e = kvp::launch_linear_decode(a, list, n, head_dim, reinterpret_cast<hipStream_t>(stream));
+  }
+  return e == hipSuccess ? KVP_OK : hip_err(e, "linear_decode_attn launch");
+} catch (const std::exception& x) {
+  return set_err(KVP_ENOMEM, "linear_decode_attn: %s", x.what());
 }
 
 int kv_gather(kvp_pool_t pool, int layer, const int32_t* block_tables, int maxp, const int32_t* lens, int num_seqs,

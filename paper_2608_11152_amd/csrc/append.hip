@@ -6,6 +6,7 @@
 // writes are whole 16-byte chunks of a single 8 KB page block.
 #include "kvp_kernels.h"
 #include "kvp_layout.h"
+#include "rope_dev.h"
 
 namespace kvp {
 
@@ -239,6 +240,64 @@ __global__ __launch_bounds__(256) void gather_kernel(GatherArgs a) {
   }
 }
 
+// kv_append_rope: one wave per (page run, head), the KV heads first, then the query heads of the same tokens.  A lane
+// turns pairs of one head's dims; a dim that is not rotated is a unit of its own.
+template <int D, bool F8>
+__global__ __launch_bounds__(256) void append_rope_kernel(AppendRopeArgs r) {
+  const AppendArgs& a = r.kv;
+  const int lane = threadIdx.x & 63;
+  const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int heads = a.Hkv + r.Hq, run = (int)(unit / heads), h = (int)(unit - (int64_t)run * heads);
+  if (run >= a.n_runs) return;
+  const PageRun pr = a.runs[run];
+  const int ntok = pr.s_hi - pr.s_lo;
+  const bool key = h < a.Hkv;
+  int64_t block = 0;
+  if (key) {
+    const int id = a.bt[(int64_t)pr.row * a.maxp + pr.lpage];
+    if ((unsigned)id >= (unsigned)a.num_pages) {
+      if (lane == 0) atomicCAS(a.err, 0, KVP_ERANGE);
+      return;
+    }
+    block = ((int64_t)id * a.Hkv + h) * (2 * 16 * D);
+  }
+  uint8_t* const b8 = reinterpret_cast<uint8_t*>(a.layer) + block;
+  uint16_t* const b16 = a.layer + block;
+  const int R = r.table.rotary_dim, units = D - R / 2;
+  for (int e = lane; e < ntok * units; e += 64) {
+    const int tt = e / units, u = e - tt * units, s = pr.s_lo + tt;
+    const int64_t tok = pr.src0 + tt;
+    const uint16_t* x = key ? a.k + tok * r.k_stride + h * D : r.q + tok * r.q_stride + (h - a.Hkv) * D;
+    const bool pair = u < R / 2;
+    const int i0 = !pair ? u + R / 2 : r.table.interleaved ? 2 * u : u;
+    const int i1 = !pair ? i0 : r.table.interleaved ? 2 * u + 1 : u + R / 2;
+    float y0 = widen(x[i0]), y1 = y0;
+    if (pair) {
+      float sn, cs;
+      pair_turn(r.table, u, pr.lpage * 16 + s, &sn, &cs);
+      turn(y0, widen(x[i1]), sn, cs, &y0, &y1);
+    }
+    if (!key) {
+      uint16_t* o = r.q_out + tok * r.q_out_stride + (h - a.Hkv) * D;
+      o[i0] = narrow(y0);
+      o[i1] = narrow(y1);
+    } else if (F8) {
+      b8[k8_index<D>(s, i0)] = (uint8_t)e4m3_code(y0 * a.inv_scale_k);
+      b8[k8_index<D>(s, i1)] = (uint8_t)e4m3_code(y1 * a.inv_scale_k);
+    } else {
+      b16[k_index<D>(s, i0)] = narrow(y0);
+      b16[k_index<D>(s, i1)] = narrow(y1);
+    }
+  }
+  if (!key) return;
+  for (int e = lane; e < ntok * D; e += 64) {
+    const int tt = e / D, c = e - tt * D, s = pr.s_lo + tt;
+    const uint16_t v = a.v[(pr.src0 + tt) * r.v_stride + h * D + c];
+    if (F8) b8[16 * D + v8_index<D>(s, c)] = (uint8_t)e4m3_code(widen(v) * a.inv_scale_v);
+    else b16[16 * D + v_index<D>(s, c)] = v;
+  }
+}
+
 __global__ void fill_zero_kernel(uint4* p, size_t n16) {
   const size_t stride = (size_t)gridDim.x * blockDim.x;
   for (size_t i = (size_t)blockIdx.x * blockDim.x + threadIdx.x; i < n16; i += stride) p[i] = make_uint4(0, 0, 0, 0);
@@ -269,6 +328,21 @@ hipError_t launch_append(const AppendArgs& a, int D, hipStream_t s) {
     hipLaunchKernelGGL(append_kernel<128>, grid, dim3(256), 0, s, a);
   } else {
     hipLaunchKernelGGL(append_kernel<64>, grid, dim3(256), 0, s, a);
+  }
+  return hipGetLastError();
+}
+
+hipError_t launch_append_rope(const AppendRopeArgs& a, int D, hipStream_t s) {
+  const int64_t units = (int64_t)a.kv.n_runs * (a.kv.Hkv + a.Hq);
+  if (units == 0) return hipSuccess;
+  const dim3 grid((unsigned)((units + 3) / 4));
+  if (a.kv.fp8) {
+    if (D == 128) hipLaunchKernelGGL((append_rope_kernel<128, true>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((append_rope_kernel<64, true>), grid, dim3(256), 0, s, a);
+  } else if (D == 128) {
+    hipLaunchKernelGGL((append_rope_kernel<128, false>), grid, dim3(256), 0, s, a);
+  } else {
+    hipLaunchKernelGGL((append_rope_kernel<64, false>), grid, dim3(256), 0, s, a);
   }
   return hipGetLastError();
 }

@@ -31,6 +31,66 @@ struct AppendArgs {
   float inv_scale_k, inv_scale_v;
 };
 
+// The rotation of kvp_rope, passed to kernels by value.
+constexpr int kRopePairs = 128;
+struct RopeTable {
+  uint64_t turns[kRopePairs];  // 2^64 * turns per position of each pair
+  int32_t rotary_dim, interleaved;
+  float magnitude;
+};
+
+struct RopeArgs {
+  RopeTable table;
+  const void* x;            // token t, head h at x + t * x_token + h * x_head elements, D of them
+  void* y;
+  int64_t x_token, x_head, y_token, y_head;
+  const int32_t* pos;       // [tokens]
+  int64_t tokens;
+  int heads, D;
+  int grad;                 // the transpose
+};
+
+struct AppendRopeArgs {
+  AppendArgs kv;            // k and v rows at the strides below
+  RopeTable table;
+  int64_t k_stride, v_stride;  // elements from token to token
+  const uint16_t* q;        // [T, Hq, D] at q_stride; Hq = 0: none
+  uint16_t* q_out;
+  int64_t q_stride, q_out_stride;
+  int Hq;
+};
+
+// Linear attention over states [slots, Hkv, D, D].  One item is a run of tokens of one sequence.
+struct LinearItem {
+  int32_t t0, n;            // first token, tokens
+  int32_t src, dst;         // state slots; -1: starts from zeros / is not kept
+};
+
+// Items and decay rates travel in the launch arguments (linear_decode_attn reads no host memory later).
+constexpr int kLinearBatch = 192, kLinearHeads = 128;
+struct LinearList {
+  LinearItem items[kLinearBatch];
+  float decay[kLinearHeads];
+};
+
+// The same in pinned host memory (linear_chunk_attn).
+struct LinearItems {
+  const LinearItem* items;
+  const float* decay;
+};
+
+struct LinearArgs {
+  const uint16_t* q;        // [T, Hq, D] at q_stride elements from token to token
+  const uint16_t* k;        // [T, Hkv, D]
+  const uint16_t* v;
+  int64_t q_stride, k_stride, v_stride;
+  float* state;
+  void* out;                // [T, Hq, D]
+  int out_f32;
+  int Hq, Hkv;
+  float scale;
+};
+
 struct GatherArgs {
   uint16_t* k;              // [T, Hkv, D] out
   uint16_t* v;
@@ -159,6 +219,10 @@ struct TableArgs {
 };
 
 hipError_t launch_append(const AppendArgs& a, int D, hipStream_t s);
+hipError_t launch_append_rope(const AppendRopeArgs& a, int D, hipStream_t s);
+hipError_t launch_rope(const RopeArgs& a, bool f32, hipStream_t s);
+hipError_t launch_linear_decode(const LinearArgs& a, const LinearList& list, int n_items, int D, hipStream_t s);
+hipError_t launch_linear_chunk(const LinearArgs& a, const LinearItems& list, int n_items, int D, hipStream_t s);
 hipError_t launch_gather(const GatherArgs& a, int D, hipStream_t s);
 hipError_t launch_fill_zero(void* p, size_t bytes, hipStream_t s);
 // Copy n bytes from pinned host memory (src) to device memory (dst; 16-byte aligned, like src) with a

@@ -29,7 +29,8 @@ EXPORTS = ["kv_pool_create", "kv_pool_destroy", "kv_pool_reset", "kv_pool_layer_
            "kv_restore", "kvp_block_hashes", "kvp_group_shared_pages", "kvp_prefix_table_create",
            "kvp_prefix_table_destroy", "kvp_prefix_table_clear", "kvp_prefix_table_insert", "kvp_prefix_table_erase",
            "kvp_prefix_lookup", "kvp_prefix_table_error", "kvp_check_tables",
-           "kvp_plan_decode", "kvp_strerror", "kvp_last_error", "kvp_version"]
+           "kvp_plan_decode", "kvp_rope_init", "kvp_rope_apply", "kv_append_rope", "linear_chunk_workspace_size",
+           "linear_chunk_attn", "linear_decode_attn", "kvp_strerror", "kvp_last_error", "kvp_version"]
 
 
 class KvpError(RuntimeError):
@@ -41,6 +42,15 @@ class KvpError(RuntimeError):
 class GroupPrefix(C.Structure):
     _fields_ = [("group_id", C.POINTER(C.c_int32)), ("shared_pages", C.POINTER(C.c_int32)),
                 ("num_groups", C.c_int32)]
+
+
+ROPE_PAIRS = 128  # KVP_ROPE_PAIRS
+LINEAR_MAX_HEADS = 128  # KVP_LINEAR_MAX_HEADS
+
+
+class RopeStruct(C.Structure):
+    _fields_ = [("rotary_dim", C.c_int32), ("interleaved", C.c_int32), ("magnitude", C.c_float), ("valid", C.c_int32),
+                ("turns", C.c_uint64 * ROPE_PAIRS)]
 
 
 _lib = None
@@ -88,6 +98,15 @@ def lib() -> C.CDLL:
         L.kvp_prefix_table_error.argtypes = [p, C.POINTER(i)]
         L.kvp_check_tables.argtypes = [i32p, i, i32p, i, i, gpp]
         L.kvp_plan_decode.argtypes = [i32p, i, gpp, i, i, i32p, i, C.POINTER(i), C.POINTER(i), C.POINTER(i)]
+        rp, f32p, i64, dbl = C.POINTER(RopeStruct), C.POINTER(C.c_float), C.c_int64, C.c_double
+        L.kvp_rope_init.argtypes = [rp, i, i, dbl, dbl, i, dbl, dbl, dbl]
+        L.kvp_rope_apply.argtypes = [rp, vp, i64, i64, vp, i64, i64, i, vp, i64, i, i, i, vp]
+        L.kv_append_rope.argtypes = [p, i, rp, vp, i64, vp, i64, vp, i64, vp, i64, i, vp, i, i32p, i32p, i, gpp, vp]
+        L.linear_chunk_workspace_size.argtypes = [i32p, i, i, i, C.POINTER(sz)]
+        L.linear_chunk_attn.argtypes = [vp, i64, vp, i64, vp, i64, vp, i, f32p, i32p, i32p, i32p, i, i, i, i, C.c_float,
+                                        vp, i, vp, sz, vp]
+        L.linear_decode_attn.argtypes = [vp, i64, vp, i64, vp, i64, vp, i, f32p, i32p, i32p, i, i, i, i, C.c_float, vp, i,
+                                         vp]
         L.kvp_strerror.argtypes = [i]
         L.kvp_strerror.restype = C.c_char_p
         L.kvp_last_error.restype = C.c_char_p
@@ -199,6 +218,35 @@ def _dev(t, name: str, dtypes, ndim: int | None = None, rows: int | None = None,
     return t
 
 
+def _heads(t, name: str, dtypes, rows: int | None = None):
+    """A [tokens, heads, head_dim] tensor whose heads may lie apart (rows of a fused projection, for instance) while
+    the elements of a head are dense, on the current device."""
+    import torch
+    if not getattr(t, "is_cuda", False):
+        raise ValueError(f"{name} must be a GPU tensor")
+    if t.dtype not in dtypes:
+        raise ValueError(f"{name} has dtype {t.dtype}; expected one of {', '.join(str(d) for d in dtypes)}")
+    if t.dim() != 3:
+        raise ValueError(f"{name} has {t.dim()} dimensions, expected 3")
+    if t.shape[2] > 1 and t.stride(2) != 1:
+        raise ValueError(f"{name}'s head elements must be contiguous")
+    if rows is not None and t.shape[0] < rows:
+        raise ValueError(f"{name} has {t.shape[0]} rows, {rows} needed")
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} is on device {t.device.index}, the current device is {torch.cuda.current_device()}")
+    return t
+
+
+def _rows(t, name: str, rows: int, heads: int | None = None, d: int | None = None) -> int:
+    """Checks a bf16 [tokens, heads, d] tensor whose tokens may lie apart; returns the stride between them."""
+    _heads(t, name, _bf16(), rows)
+    if (heads is not None and t.shape[1] != heads) or (d is not None and t.shape[2] != d):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected (*, {heads}, {d})")
+    if t.shape[1] > 1 and t.stride(1) != t.shape[2]:
+        raise ValueError(f"{name}'s heads must be contiguous")
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+
+
 def _bf16():
     import torch
     return (torch.bfloat16,)
@@ -307,6 +355,134 @@ def kv_append(pool: Pool, layer, k, v, block_tables, start_pos, cu_new, group_pr
         _dev(v, "v", _bf16(), 3, rows=int(cu[-1]), tail=tail)
     _check(lib().kv_append(pool.handle, layer, _dptr(k), _dptr(v), _dptr(block_tables), block_tables.shape[1],
                            _ptr(sp), _ptr(cu), len(sp), _gp_ref(group_prefix), _stream(stream)), "kv_append")
+
+
+class Rope:
+    """A rotation of the first `rotary_dim` dims of a head by position (kvp_rope_init): half or interleaved pairs,
+    frequencies scaled for contexts `factor` times `original_len` (0: every frequency divided by factor)."""
+
+    def __init__(self, rotary_dim: int, base: float = 10000.0, interleaved: bool = False, factor: float = 1.0,
+                 original_len: int = 0, low_turns: float = 1.0, high_turns: float = 32.0, magnitude: float = 1.0):
+        self.s = RopeStruct()
+        _check(lib().kvp_rope_init(C.byref(self.s), rotary_dim, int(interleaved), base, factor, original_len, low_turns,
+                                   high_turns, magnitude), "kvp_rope_init")
+        self.rotary_dim = rotary_dim
+
+    def ref(self):
+        return C.byref(self.s)
+
+
+def kvp_rope_apply(rope: Rope, x, positions, out=None, grad: bool = False, stream=None):
+    """The heads of x [T, H, d] (bf16 or fp32, tokens and heads at any stride) turned by positions (device int32 [T]);
+    grad: the transpose, for the gradient.  `out` may be x; a new tensor is dense."""
+    import torch
+    dtypes = (torch.bfloat16, torch.float32)
+    _heads(x, "x", dtypes)
+    T, H, d = x.shape
+    _dev(positions, "positions", _i32t(), 1, rows=T)
+    if positions.device != x.device:
+        raise ValueError(f"positions is on {positions.device}, x on {x.device}")
+    if out is None:
+        out = _alloc_on(stream, (T, H, d), x.dtype, x.device)
+    else:
+        _heads(out, "out", (x.dtype,))
+        if out.shape != x.shape:
+            raise ValueError(f"out has shape {tuple(out.shape)}, x {tuple(x.shape)}")
+    _check(lib().kvp_rope_apply(rope.ref(), _dptr(x), x.stride(0), x.stride(1), _dptr(out), out.stride(0), out.stride(1),
+                                KVP_F32 if x.dtype == torch.float32 else KVP_BF16, _dptr(positions), T, H, d, int(grad),
+                                _stream(stream)), "kvp_rope_apply")
+    return out
+
+
+def kv_append_rope(pool: Pool, layer, rope: Rope, k, v, block_tables, start_pos, cu_new, q=None, q_out=None,
+                   group_prefix=None, stream=None):
+    """kv_append with the keys turned to their positions, and with q [T, Hq, d] the same tokens' queries, returned (in
+    `q_out`, which may be q).  k, v, q: device bf16, tokens at any stride that is a multiple of 8 elements."""
+    sp, cu = _i32(start_pos), _i32(cu_new)
+    if len(cu) != len(sp) + 1:
+        raise ValueError(f"cu_new has {len(cu)} entries, {len(sp) + 1} needed")
+    _dev(block_tables, "block_tables", _i32t(), 2, rows=len(sp))
+    T = int(cu[-1]) if len(sp) else 0
+    ks = _rows(k, "k", T, pool.num_kv_heads, pool.head_dim)
+    vs = _rows(v, "v", T, pool.num_kv_heads, pool.head_dim)
+    Hq = qs = os_ = 0
+    if q is not None:
+        Hq = q.shape[1] if q.dim() == 3 else 0
+        qs = _rows(q, "q", T, Hq, pool.head_dim)
+        if q_out is None:
+            q_out = _alloc_on(stream, tuple(q.shape), q.dtype, q.device)
+        os_ = _rows(q_out, "q_out", T, Hq, pool.head_dim)
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    _check(lib().kv_append_rope(pool.handle, layer, rope.ref(), _dptr(k), ks, _dptr(v), vs, _dptr(q), qs, _dptr(q_out),
+                                os_, Hq, _dptr(block_tables), block_tables.shape[1], _ptr(sp), _ptr(cu), len(sp),
+                                _gp_ref(group_prefix), _stream(stream)), "kv_append_rope")
+    return q_out
+
+
+def _linear_args(q, k, v, state, decay, src_slots, dst_slots, rows, scale, out, out_dtype, stream):
+    """Checks and arguments that both linear attention calls share: (pointers and strides, host arrays, shape, out)."""
+    import torch
+    dec = np.ascontiguousarray(np.asarray(decay, dtype=np.float32))
+    src, dst = _i32(src_slots), _i32(dst_slots)
+    if src.shape != dst.shape or src.ndim != 1:
+        raise ValueError(f"src_slots has shape {src.shape}, dst_slots {dst.shape}: one slot per sequence each")
+    qs = _rows(q, "q", rows)
+    T, Hq, d = q.shape
+    ks = _rows(k, "k", rows, d=d, heads=k.shape[1] if k.dim() == 3 else None)
+    Hkv = k.shape[1]
+    vs = _rows(v, "v", rows, Hkv, d)
+    if dec.shape != (Hkv,):
+        raise ValueError(f"decay has shape {dec.shape}, k {Hkv} heads")
+    _dev(state, "state", (torch.float32,), 4, tail=(Hkv, d, d))
+    if out is None:
+        out = _alloc_on(stream, (T, Hq, d), out_dtype or torch.float32, q.device)
+    _dev(out, "out", _outt(), 3, rows=rows, tail=(Hq, d))
+    if state.device != q.device or out.device != q.device:
+        raise ValueError(f"q is on {q.device}, state on {state.device}, out on {out.device}")
+    if scale is None:
+        scale = 1.0 / math.sqrt(d)
+    head = (_dptr(q), qs, _dptr(k), ks, _dptr(v), vs, _dptr(state), state.shape[0],
+            dec.ctypes.data_as(C.POINTER(C.c_float)), _ptr(src), _ptr(dst))
+    tail = (len(src), Hq, Hkv, d, float(scale), _dptr(out), KVP_F32 if out.dtype == torch.float32 else KVP_BF16)
+    return head, tail, out, (dec, src, dst)
+
+
+def linear_chunk_workspace_size(cu, num_kv_heads: int, head_dim: int) -> int:
+    cu = _i32(cu)
+    n = C.c_size_t()
+    _check(lib().linear_chunk_workspace_size(_ptr(cu), len(cu) - 1, num_kv_heads, head_dim, C.byref(n)),
+           "linear_chunk_workspace_size")
+    return n.value
+
+
+def linear_chunk_attn(q, k, v, state, decay, src_slots, dst_slots, cu, scale=None, out=None, out_dtype=None, ws=None,
+                      stream=None):
+    """Linear attention of ragged chunks: q [T, Hq, d], k, v [T, Hkv, d] device bf16 (tokens at any stride that is a
+    multiple of 8 elements), state device fp32 [slots, Hkv, d, d]; decay, src_slots, dst_slots, cu host."""
+    import torch
+    cu = _i32(cu)
+    if len(cu) != len(_i32(src_slots)) + 1:
+        raise ValueError(f"cu has {len(cu)} entries, {len(_i32(src_slots)) + 1} needed")
+    head, tail, out, keep = _linear_args(q, k, v, state, decay, src_slots, dst_slots, int(cu[-1]), scale, out, out_dtype,
+                                         stream)
+    if ws is None:
+        ws = _alloc_on(stream, max(1, linear_chunk_workspace_size(cu, k.shape[1], k.shape[2])), torch.uint8, q.device)
+    _dev(ws, "ws", (ws.dtype,))
+    _check(lib().linear_chunk_attn(*head, _ptr(cu), *tail, _dptr(ws), ws.numel() * ws.element_size(), _stream(stream)),
+           "linear_chunk_attn")
+    return out
+
+
+def linear_decode_attn(q, k, v, state, decay, src_slots, dst_slots, scale=None, out=None, out_dtype=None, stream=None):
+    """Linear attention of one token per sequence: row i of q [B, Hq, d], k, v [B, Hkv, d]; the rest as in
+    linear_chunk_attn."""
+    head, tail, out, keep = _linear_args(q, k, v, state, decay, src_slots, dst_slots, len(src_slots), scale, out,
+                                         out_dtype, stream)
+    if q.shape[0] != len(src_slots):
+        raise ValueError(f"q holds {q.shape[0]} sequences, src_slots {len(src_slots)}")
+    _check(lib().linear_decode_attn(*head, *tail, _stream(stream)), "linear_decode_attn")
+    return out
 
 
 def kv_gather(pool: Pool, layer, block_tables, lens, stream=None):
