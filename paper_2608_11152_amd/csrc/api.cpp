@@ -614,6 +614,8 @@ int check_cu(const int32_t* cu, int num_seqs) {
   return KVP_OK;
 }
 
+constexpr int64_t kLinearMaxStride = 1 << 24;
+
 constexpr int32_t kRopeValid = 0x726f7065;  // kvp_rope.valid
 
 // Rows of bf16 that a kernel reads or writes 16 bytes at a time.
@@ -1006,6 +1008,9 @@ int linear_chunk_attn(const void* q, int64_t q_stride, const void* k, int64_t k_
     rc = check_linear(q, q_stride, k, k_stride, v, v_stride, state, num_slots, decay, src_slots, dst_slots, num_seqs,
                       cu[num_seqs] > 0, num_q_heads, num_kv_heads, head_dim, scale, out, out_dtype);
   if (rc) return rc;
+  for (const int64_t stride : {q_stride, k_stride, v_stride})  // the kernel reads a chunk's rows at 32-bit offsets
+    if (cu[num_seqs] > 0 && (stride < head_dim || stride > kLinearMaxStride))
+      return set_err(KVP_EINVAL, "stride %lld outside [head_dim, %lld]", (long long)stride, (long long)kLinearMaxStride);
   std::vector<kvp::LinearItem> items;
   for (int i = 0; i < num_seqs; ++i) items.push_back({cu[i], cu[i + 1] - cu[i], src_slots[i], dst_slots[i]});
   const kvp::LinearArgs a = linear_args(q, q_stride, k, k_stride, v, v_stride, state, num_q_heads, num_kv_heads, scale,

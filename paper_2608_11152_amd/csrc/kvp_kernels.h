@@ -85,6 +85,7 @@ struct LinearArgs {
   const uint16_t* v;
   int64_t q_stride, k_stride, v_stride;
   float* state;
+  float* parts;             // states of parts of long sequences (workspace)
   void* out;                // [T, Hq, D]
   int out_f32;
   int Hq, Hkv;

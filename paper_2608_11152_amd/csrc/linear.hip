@@ -1,11 +1,374 @@
 // Linear attention with a decay per head over a state per session:
 //   S_t = decay S_{t-1} + k_t v_t^T,   o_t = scale q_t^T S_t
-// q, k, v bf16, the state and every sum fp32; the output is rounded once.  The recurrence itself: one workgroup per
-// (item, KV head), thread c holds column c of the state in registers and walks the item's tokens.
+// q, k, v bf16, the state and every sum fp32; the output is rounded once.
+//
+// linear_step_kernel: the recurrence itself for single tokens: one workgroup per (sequence, KV head), thread c holds
+// column c of the state in registers.
+//
+// linear_chunk_kernel: chunks of 64 tokens, from the state S before the chunk (rows i, j of the chunk, l = decay):
+//   O = (l^(i+1) Q) S + (Q K^T . l^(i-j) for j <= i) V          S' = l^64 S + (l^(63-j) K)^T V
+// One workgroup of 2 D threads per (item, KV head) walks an item's tokens; each of its D / 32 waves holds 32 columns of
+// S in registers (fp32, 2 D registers' worth per 4 rows) from the first chunk to the last, so a chunk reads q, k, v and
+// writes o, once.  Bandwidth is what bounds it: 8 D bytes and 6 D^2 .. 10 D^2 flops a token and head.
+//
+// All products run as v_mfma_f32_16x16x32_bf16.  Its result tile gives a lane 4 rows (4 g + r) of one column; its
+// operand wants 8 consecutive k of one row or column.  Two stacked result tiles are such an operand if k is read in the
+// order  slot(8 g + b) = 4 g + b, slot(8 g + 4 + b) = 16 + 4 g + b  (b < 4): the sum over k does not mind.  So the
+// dims of Q and K and the tokens of K^T and V^T lie in that order in LDS, and the state and the weights of a chunk go
+// from one product's result into the next one's operand without leaving their registers:
+//   P^T (keys x rows)   = K Q^T           O^T (columns x rows) = S^T Q^T + V^T P^T           S (dims x columns) = K^T V
+// Each wave computes all of P^T (a tenth of its matrix work) rather than share it through LDS and a barrier.
+//
+// Operands that are not bf16 are carried as sums of bf16 parts: S and P as two (2^-18 left: far inside a bf16 output's
+// half step 2^-9), the decayed V that goes into the state as three (2^-26: the state is fp32).
+#include <algorithm>
+
 #include "rope_dev.h"
 
 namespace kvp {
 namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+__device__ __forceinline__ unsigned pack2(float lo, float hi) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  bf16x2 v;
+  v[0] = (__bf16)lo;
+  v[1] = (__bf16)hi;
+  return __builtin_bit_cast(unsigned, v);
+}
+__device__ __forceinline__ float low(unsigned w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float high(unsigned w) { return __uint_as_float(w & 0xffff0000u); }
+
+// The bf16 of x and y, packed; x and y become what is left of them.
+__device__ __forceinline__ unsigned part(float& x, float& y) {
+  const unsigned w = pack2(x, y);
+  x -= low(w);
+  y -= high(w);
+  return w;
+}
+
+// x, as a value that the compiler does not know: reads at it are made again instead of held in registers.
+__device__ __forceinline__ int again(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
+// Position of element x of a 32 block in the order of the operands above.
+__device__ __forceinline__ int slot_of(int x) { return ((x >> 2) & 3) * 8 + ((x >> 4) & 1) * 4 + (x & 3); }
+
+__device__ double power(double x, unsigned n) {
+  double y = 1.0;
+  for (; n; n >>= 1, x *= x)
+    if (n & 1) y *= x;
+  return y;
+}
+
+constexpr int kChunk = 64;  // tokens
+
+template <int D>
+struct Tiles {
+  uint16_t q[kChunk][D + 8];   // rows of tokens, dims in slot order.  The 16 bytes behind each row spread the 16 rows
+  uint16_t k[kChunk][D + 8];   // that a wave reads at a time over all banks
+  uint16_t kt[D][kChunk + 8];  // rows of dims, tokens in slot order
+  uint16_t vt[D][kChunk + 8];
+  float pw[kChunk + 1];        // decay^n
+};
+
+// 8 rows (tokens) of 8 elements become 8 rows (dims) of 8 tokens, and go to LDS.
+template <int P>
+__device__ __forceinline__ void store_transposed(uint16_t (*dst)[P], int dim, int at, const u32x4* row) {
+#pragma unroll
+  for (int d = 0; d < 8; ++d) {
+    u32x4 w;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      w[j] = __builtin_amdgcn_perm(row[2 * j + 1][d >> 1], row[2 * j][d >> 1], d & 1 ? 0x07060302u : 0x05040100u);
+    *reinterpret_cast<u32x4*>(&dst[dim + d][at]) = w;
+  }
+}
+
+// 8 dims of one token, in slot order: two pieces of 4.
+template <int P>
+__device__ __forceinline__ void store_row(uint16_t (*dst)[P], int token, int dim, u32x4 v) {
+  uint16_t* p = &dst[token][(dim & ~31) + slot_of(dim & 31)];
+  *reinterpret_cast<u32x2*>(p) = u32x2{v[0], v[1]};
+  *reinterpret_cast<u32x2*>(p + 8) = u32x2{v[2], v[3]};
+}
+
+__device__ __forceinline__ u32x4 ld16(const uint16_t* p) { return *reinterpret_cast<const u32x4*>(p); }
+
+// Up to a chunk's rows of one head, as a buffer: reads behind the last row give zeros, writes there are dropped.
+struct Rows {
+  __amdgpu_buffer_rsrc_t rsrc;
+  __device__ __forceinline__ Rows(const void* p, int64_t stride, int rows, int D, int bytes = 2)
+      : rsrc(__builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0,
+                                               rows > 0 ? ((min(rows, kChunk) - 1) * (int)stride + D) * bytes : 0,
+                                               0x00020000)) {}
+  __device__ __forceinline__ u32x4 load(int at) const { return __builtin_amdgcn_raw_buffer_load_b128(rsrc, at, 0, 0); }
+  __device__ __forceinline__ void store(int at, u32x4 v) const {
+    __builtin_amdgcn_raw_buffer_store_b128(v, rsrc, at, 0, 0);
+  }
+};
+
+// State of an item: a slot of the caller's, a part of the workspace (-2, -3, ..), or none (-1).
+__device__ __forceinline__ float* state_at(const LinearArgs& a, int slot, int h, int D) {
+  float* base = slot >= 0 ? a.state : a.parts;
+  return base + ((int64_t)(slot >= 0 ? slot : -2 - slot) * a.Hkv + h) * D * D;
+}
+
+// kAttend: outputs and state; otherwise only the state, from zeros (the sum of a part of a long sequence).
+template <int D, bool kAttend>
+__global__ __launch_bounds__(2 * D, 2) void linear_chunk_kernel(LinearArgs a, LinearItems list) {
+  __shared__ Tiles<D> L;
+  constexpr int KS = D / 32, MT = D / 16;  // k-steps and row tiles over the dims of k
+  const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, m = lane & 15, g = lane >> 4;
+  const int item = blockIdx.x / a.Hkv, h = blockIdx.x - item * a.Hkv, G = kAttend ? a.Hq / a.Hkv : 1;
+  const LinearItem it = list.items[item];
+  const double l1 = (double)list.decay[h];
+  if (tid <= kChunk) L.pw[tid] = (float)power(l1, tid);
+
+  // Column n of the wave's 16-wide tile nt is column 8 (n / 4) + 4 nt + n % 4 of its 32: a lane's rows of O^T from
+  // both tiles are then 8 consecutive columns.
+  const int col = 32 * w + 8 * (m >> 2) + (m & 3);
+  f32x4 S[MT][2];
+  {
+    const float* from = it.src == -1 ? nullptr : state_at(a, it.src, h, D);
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) S[mt][nt][r] = from ? from[(16 * mt + 4 * g + r) * D + col + 4 * nt] : 0.0f;
+  }
+
+  // What a thread brings: an 8 x 8 block of k (the first D threads) or v, and 4 pieces of q.  Rows behind the item's
+  // last are outside their buffer and read as zeros.
+  const int c8 = (tid % (D / 8)) * 8, tg = (tid % D) / (D / 8), first = 32 * (tg >> 2) + 4 * (tg & 3);
+  const bool keys = w < D / 64;
+  const uint16_t* const kv = keys ? a.k : a.v;
+  const int64_t kv_stride = keys ? a.k_stride : a.v_stride;
+  const int qrow = tid / (D / 8);
+  u32x4 rkv[8], rq[4];
+  auto fetch_kv = [&](int c) {
+    const Rows rows(kv + (it.t0 + (int64_t)c) * kv_stride + h * D, kv_stride, it.n - c, D);
+    const int at = again(2 * (first * (int)kv_stride + c8));
+#pragma unroll
+    for (int j = 0; j < 8; ++j) rkv[j] = rows.load(at + 2 * ((j & 3) + 4 * (j & 4)) * (int)kv_stride);
+  };
+  auto fetch_q = [&](int c, int gq) {
+    const Rows rows(a.q + (it.t0 + (int64_t)c) * a.q_stride + (h * G + gq) * D, a.q_stride, it.n - c, D);
+    const int at = again(2 * (qrow * (int)a.q_stride + c8));
+#pragma unroll
+    for (int j = 0; j < 4; ++j) rq[j] = rows.load(at + 32 * j * (int)a.q_stride);
+  };
+  fetch_kv(0);
+  if (kAttend) fetch_q(0, 0);
+
+  // The state's decay over a chunk, l^64 rounded to fp32, would be off the same way at every chunk.  `off` is the
+  // product of the factors so far over the true one, within a step of fp32 of 1; each factor takes it back.
+  const double l64 = power(l1, kChunk), back = 1.0 / l64;
+  const bool track = l64 > 1e-30;
+  double off = 1.0;
+
+  for (int c = 0; c < it.n; c += kChunk) {
+    const int n = min(kChunk, it.n - c);
+    for (int gq = 0; gq < G; ++gq) {
+      __syncthreads();
+      if (gq == 0) {
+        if (keys) {
+          store_transposed(L.kt, c8, 32 * (tg >> 2) + 8 * (tg & 3), rkv);
+          if (kAttend)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) store_row(L.k, first + (j & 3) + 4 * (j & 4), c8, rkv[j]);
+        } else {
+          store_transposed(L.vt, c8, 32 * (tg >> 2) + 8 * (tg & 3), rkv);
+        }
+      }
+      if (kAttend)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) store_row(L.q, qrow + 16 * j, c8, rq[j]);
+      __syncthreads();
+      if (gq == G - 1) {
+        fetch_kv(c + kChunk);
+        if (kAttend) fetch_q(c + kChunk, 0);
+      } else {
+        fetch_q(c, gq + 1);
+      }
+      if (kAttend) {
+        // O^T = S^T Q^T for the chunk's four row tiles
+        f32x4 O[4][2] = {};
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          __builtin_amdgcn_sched_barrier(0);
+          u32x4 qf[4];
+#pragma unroll
+          for (int rt = 0; rt < 4; ++rt) qf[rt] = ld16(&L.q[16 * rt + m][32 * ks + 8 * g]);
+#pragma unroll
+          for (int nt = 0; nt < 2; ++nt) {
+            u32x4 hi, lo;
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+              float x = S[2 * ks + (b >> 1)][nt][2 * (b & 1)], y = S[2 * ks + (b >> 1)][nt][2 * (b & 1) + 1];
+              hi[b] = part(x, y);
+              lo[b] = pack2(x, y);
+            }
+#pragma unroll
+            for (int rt = 0; rt < 4; ++rt) {
+              O[rt][nt] = mfma16(hi, qf[rt], O[rt][nt]);
+              O[rt][nt] = mfma16(lo, qf[rt], O[rt][nt]);
+            }
+          }
+        }
+        const int es = a.out_f32 ? 4 : 2;
+        const Rows out(reinterpret_cast<char*>(a.out) + ((it.t0 + (int64_t)c) * a.Hq + h * G + gq) * D * es, a.Hq * D,
+                       n, D, es);
+        bool bad = false;
+#pragma unroll
+        for (int rt = 3; rt >= 0; --rt) {
+          __builtin_amdgcn_sched_barrier(0);
+          // P^T: lane column m is row i = 16 rt + m, its rows are keys j = 16 jt + 4 g + r
+          const int g8 = again(8 * g), m4 = again(m - 4 * g);
+          f32x4 P[4] = {};
+#pragma unroll
+          for (int ks = 0; ks < KS; ++ks) {
+            const u32x4 qf = ld16(&L.q[16 * rt + m][32 * ks + g8]);
+#pragma unroll
+            for (int jt = 0; jt <= rt; ++jt) P[jt] = mfma16(ld16(&L.k[16 * jt + m][32 * ks + g8]), qf, P[jt]);
+          }
+#pragma unroll
+          for (int jt = 0; jt <= rt; ++jt)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const int e = m4 + 16 * (rt - jt) - r;
+              if (jt < rt) P[jt][r] *= a.scale * L.pw[e];
+              else P[jt][r] = e >= 0 ? P[jt][r] * (a.scale * L.pw[max(e, 0)]) : 0.0f;
+            }
+          f32x4 V[2] = {};
+#pragma unroll
+          for (int s = 0; s <= rt / 2; ++s) {
+            u32x4 hi, lo;
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+              float x = P[2 * s + (b >> 1)][2 * (b & 1)], y = P[2 * s + (b >> 1)][2 * (b & 1) + 1];
+              hi[b] = part(x, y);
+              lo[b] = pack2(x, y);
+            }
+#pragma unroll
+            for (int nt = 0; nt < 2; ++nt) {
+              const u32x4 vf = ld16(&L.vt[col + 4 * nt][32 * s + g8]);
+              V[nt] = mfma16(vf, hi, V[nt]);
+              V[nt] = mfma16(vf, lo, V[nt]);
+            }
+          }
+          if (rt == 3) {
+            // A value of v that is not finite gives no number in the chunk's last row, and, as 0 times it, in earlier
+            // rows that must not see it.
+            float z = 0.0f;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) z += (V[0][r] - V[0][r]) + (V[1][r] - V[1][r]);
+            if (__any(z != 0.0f)) {
+              float y = 0.0f;
+#pragma unroll 1
+              for (int s = 0; s < 4; ++s) {
+                const u32x4 v = ld16(&L.vt[32 * w + (lane >> 1)][32 * (lane & 1) + 8 * s]);
+#pragma unroll
+                for (int b = 0; b < 4; ++b) y += (low(v[b]) - low(v[b])) + (high(v[b]) - high(v[b]));
+              }
+              bad = __any(y != 0.0f);
+            }
+          }
+          const int i = 16 * rt + m;
+          if (bad) {  // key by key: only keys up to the row are multiplied at all
+            V[0] = V[1] = f32x4{};
+#pragma unroll 1
+            for (int j = 0; j < 16 * rt + 16; ++j) {
+              float p = 0.0f;
+#pragma unroll 1
+              for (int d = 0; d < D; d += 8) {
+                const u32x4 x = ld16(&L.q[i][d]), y = ld16(&L.k[j][d]);
+#pragma unroll
+                for (int b = 0; b < 4; ++b) p = fmaf(high(x[b]), high(y[b]), fmaf(low(x[b]), low(y[b]), p));
+              }
+              p *= a.scale * L.pw[max(i - j, 0)];
+#pragma unroll
+              for (int x = 0; x < 8; ++x) {
+                const float v = widen(L.vt[32 * w + 8 * g + x][(j & 32) + slot_of(j & 31)]);
+                if (j <= i) V[x >> 2][x & 3] = fmaf(p, v, V[x >> 2][x & 3]);
+              }
+            }
+          }
+          const float f = a.scale * L.pw[again(i + 1)];
+#pragma unroll
+          for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) V[nt][r] = fmaf(O[rt][nt][r], f, V[nt][r]);
+          const int at = again(i) * a.Hq * D + 32 * w + 8 * g;
+          if (a.out_f32) {
+            out.store(4 * at, __builtin_bit_cast(u32x4, V[0]));
+            out.store(4 * at + 16, __builtin_bit_cast(u32x4, V[1]));
+          } else {
+            out.store(2 * at, u32x4{pack2(V[0][0], V[0][1]), pack2(V[0][2], V[0][3]), pack2(V[1][0], V[1][1]),
+                                    pack2(V[1][2], V[1][3])});
+          }
+        }
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    const int g8 = again(8 * g);
+    // S = l^n S + (l^(n-1-j) V's rows times K^T); rows from n on are zeros
+    float keep = L.pw[n];
+    if (n == kChunk && track) {
+      keep = (float)(l64 * (2.0 - off));
+      off *= (double)keep * back;
+    }
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int nt = 0; nt < 2; ++nt) S[mt][nt] *= keep;
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      __builtin_amdgcn_sched_barrier(0);
+      float d[8];
+#pragma unroll
+      for (int b = 0; b < 8; ++b) d[b] = L.pw[max(n - 1 - (32 * s + (g8 >> 1) + (b & 3) + 4 * (b & 4)), 0)];
+#pragma unroll
+      for (int nt = 0; nt < 2; ++nt) {
+        const u32x4 vf = ld16(&L.vt[col + 4 * nt][32 * s + g8]);
+        u32x4 p0, p1, p2;
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+          float x = low(vf[b]) * d[2 * b], y = high(vf[b]) * d[2 * b + 1];
+          p0[b] = part(x, y);
+          p1[b] = part(x, y);
+          p2[b] = pack2(x, y);
+        }
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+          const u32x4 kf = ld16(&L.kt[16 * mt + m][32 * s + g8]);
+          S[mt][nt] = mfma16(kf, p2, S[mt][nt]);
+          S[mt][nt] = mfma16(kf, p1, S[mt][nt]);
+          S[mt][nt] = mfma16(kf, p0, S[mt][nt]);
+        }
+      }
+    }
+  }
+  if (it.dst == -1) return;
+  float* to = state_at(a, it.dst, h, D);
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+    for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) to[(16 * mt + 4 * g + r) * D + col + 4 * nt] = S[mt][nt][r];
+}
 
 template <int D, class List>
 __global__ __launch_bounds__(D) void linear_step_kernel(LinearArgs a, List list) {
@@ -53,9 +416,9 @@ hipError_t launch_linear_decode(const LinearArgs& a, const LinearList& list, int
 
 hipError_t launch_linear_chunk(const LinearArgs& a, const LinearItems& list, int n_items, int D, hipStream_t s) {
   if (n_items == 0) return hipSuccess;
-  const dim3 grid(n_items, a.Hkv);
-  if (D == 128) hipLaunchKernelGGL((linear_step_kernel<128, LinearItems>), grid, dim3(128), 0, s, a, list);
-  else hipLaunchKernelGGL((linear_step_kernel<64, LinearItems>), grid, dim3(64), 0, s, a, list);
+  const dim3 grid(n_items * a.Hkv);
+  if (D == 128) hipLaunchKernelGGL((linear_chunk_kernel<128, true>), grid, dim3(256), 0, s, a, list);
+  else hipLaunchKernelGGL((linear_chunk_kernel<64, true>), grid, dim3(128), 0, s, a, list);
   return hipGetLastError();
 }
 
