@@ -1013,6 +1013,8 @@ int linear_chunk_attn(const void* q, int64_t q_stride, const void* k, int64_t k_
       return set_err(KVP_EINVAL, "stride %lld outside [head_dim, %lld]", (long long)stride, (long long)kLinearMaxStride);
   std::vector<kvp::LinearItem> items;
   for (int i = 0; i < num_seqs; ++i) items.push_back({cu[i], cu[i + 1] - cu[i], src_slots[i], dst_slots[i]});
+  // longest first: the last workgroups to start are short
+  std::stable_sort(items.begin(), items.end(), [](const auto& x, const auto& y) { return x.n > y.n; });
   const kvp::LinearArgs a = linear_args(q, q_stride, k, k_stride, v, v_stride, state, num_q_heads, num_kv_heads, scale,
                                         out, out_dtype);
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);

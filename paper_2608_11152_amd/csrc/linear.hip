@@ -82,9 +82,14 @@ struct Tiles {
   float pw[kChunk + 1];        // decay^n
 };
 
+// Where piece p (8 tokens) of a row of K^T or V^T lies in its row.  Rows are 36 words apart: a wave writes one piece of
+// rows 8 apart (32 words: two bank groups without this), and reads rows m, or 8 (m / 4) + m % 4, of one tile.
+__device__ __forceinline__ int piece_at(int row, int p) { return 8 * (p ^ ((row >> 2) & 4) ^ ((row >> 5) & 3)); }
+
 // 8 rows (tokens) of 8 elements become 8 rows (dims) of 8 tokens, and go to LDS.
 template <int P>
-__device__ __forceinline__ void store_transposed(uint16_t (*dst)[P], int dim, int at, const u32x4* row) {
+__device__ __forceinline__ void store_transposed(uint16_t (*dst)[P], int dim, int piece, const u32x4* row) {
+  const int at = piece_at(dim, piece);  // dim is a multiple of 8: the same for all 8 rows
 #pragma unroll
   for (int d = 0; d < 8; ++d) {
     u32x4 w;
@@ -138,15 +143,15 @@ __global__ __launch_bounds__(2 * D, 2) void linear_chunk_kernel(LinearArgs a, Li
   // Column n of the wave's 16-wide tile nt is column 8 (n / 4) + 4 nt + n % 4 of its 32: a lane's rows of O^T from
   // both tiles are then 8 consecutive columns.
   const int col = 32 * w + 8 * (m >> 2) + (m & 3);
-  f32x4 S[MT][2];
-  {
-    const float* from = it.src == -1 ? nullptr : state_at(a, it.src, h, D);
+  f32x4 S[MT][2] = {};
+  if (it.src != -1) {
+    const float* from = state_at(a, it.src, h, D) + 4 * g * D + col;
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
       for (int nt = 0; nt < 2; ++nt)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) S[mt][nt][r] = from ? from[(16 * mt + 4 * g + r) * D + col + 4 * nt] : 0.0f;
+        for (int r = 0; r < 4; ++r) S[mt][nt][r] = from[(16 * mt + r) * D + 4 * nt];
   }
 
   // What a thread brings: an 8 x 8 block of k (the first D threads) or v, and 4 pieces of q.  Rows behind the item's
@@ -180,29 +185,22 @@ __global__ __launch_bounds__(2 * D, 2) void linear_chunk_kernel(LinearArgs a, Li
 
   for (int c = 0; c < it.n; c += kChunk) {
     const int n = min(kChunk, it.n - c);
-    for (int gq = 0; gq < G; ++gq) {
-      __syncthreads();
-      if (gq == 0) {
-        if (keys) {
-          store_transposed(L.kt, c8, 32 * (tg >> 2) + 8 * (tg & 3), rkv);
-          if (kAttend)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) store_row(L.k, first + (j & 3) + 4 * (j & 4), c8, rkv[j]);
-        } else {
-          store_transposed(L.vt, c8, 32 * (tg >> 2) + 8 * (tg & 3), rkv);
-        }
-      }
+    __syncthreads();
+    if (keys) {
+      store_transposed(L.kt, c8, tg, rkv);
       if (kAttend)
 #pragma unroll
+        for (int j = 0; j < 8; ++j) store_row(L.k, first + (j & 3) + 4 * (j & 4), c8, rkv[j]);
+    } else {
+      store_transposed(L.vt, c8, tg, rkv);
+    }
+    if (kAttend) {
+      for (int gq = 0; gq < G; ++gq) {
+        if (gq > 0) __syncthreads();
+#pragma unroll
         for (int j = 0; j < 4; ++j) store_row(L.q, qrow + 16 * j, c8, rq[j]);
-      __syncthreads();
-      if (gq == G - 1) {
-        fetch_kv(c + kChunk);
-        if (kAttend) fetch_q(c + kChunk, 0);
-      } else {
-        fetch_q(c, gq + 1);
-      }
-      if (kAttend) {
+        __syncthreads();
+        if (gq + 1 < G) fetch_q(c, gq + 1);
         // O^T = S^T Q^T for the chunk's four row tiles
         f32x4 O[4][2] = {};
 #pragma unroll
@@ -221,10 +219,9 @@ __global__ __launch_bounds__(2 * D, 2) void linear_chunk_kernel(LinearArgs a, Li
               lo[b] = pack2(x, y);
             }
 #pragma unroll
-            for (int rt = 0; rt < 4; ++rt) {
-              O[rt][nt] = mfma16(hi, qf[rt], O[rt][nt]);
-              O[rt][nt] = mfma16(lo, qf[rt], O[rt][nt]);
-            }
+            for (int rt = 0; rt < 4; ++rt) O[rt][nt] = mfma16(hi, qf[rt], O[rt][nt]);
+#pragma unroll
+            for (int rt = 0; rt < 4; ++rt) O[rt][nt] = mfma16(lo, qf[rt], O[rt][nt]);
           }
         }
         const int es = a.out_f32 ? 4 : 2;
@@ -248,8 +245,8 @@ __global__ __launch_bounds__(2 * D, 2) void linear_chunk_kernel(LinearArgs a, Li
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
               const int e = m4 + 16 * (rt - jt) - r;
-              if (jt < rt) P[jt][r] *= a.scale * L.pw[e];
-              else P[jt][r] = e >= 0 ? P[jt][r] * (a.scale * L.pw[max(e, 0)]) : 0.0f;
+              P[jt][r] *= a.scale * L.pw[jt < rt ? e : max(e, 0)];
+              if (jt == rt && e < 0) P[jt][r] = 0.0f;
             }
           f32x4 V[2] = {};
 #pragma unroll
@@ -263,7 +260,7 @@ __global__ __launch_bounds__(2 * D, 2) void linear_chunk_kernel(LinearArgs a, Li
             }
 #pragma unroll
             for (int nt = 0; nt < 2; ++nt) {
-              const u32x4 vf = ld16(&L.vt[col + 4 * nt][32 * s + g8]);
+              const u32x4 vf = ld16(&L.vt[col + 4 * nt][piece_at(col, 4 * s + (g8 >> 3))]);
               V[nt] = mfma16(vf, hi, V[nt]);
               V[nt] = mfma16(vf, lo, V[nt]);
             }
@@ -278,7 +275,7 @@ __global__ __launch_bounds__(2 * D, 2) void linear_chunk_kernel(LinearArgs a, Li
               float y = 0.0f;
 #pragma unroll 1
               for (int s = 0; s < 4; ++s) {
-                const u32x4 v = ld16(&L.vt[32 * w + (lane >> 1)][32 * (lane & 1) + 8 * s]);
+                const u32x4 v = ld16(&L.vt[32 * w + (lane >> 1)][32 * (lane & 1) + 8 * s]);  // any order will do
 #pragma unroll
                 for (int b = 0; b < 4; ++b) y += (low(v[b]) - low(v[b])) + (high(v[b]) - high(v[b]));
               }
@@ -300,7 +297,8 @@ __global__ __launch_bounds__(2 * D, 2) void linear_chunk_kernel(LinearArgs a, Li
               p *= a.scale * L.pw[max(i - j, 0)];
 #pragma unroll
               for (int x = 0; x < 8; ++x) {
-                const float v = widen(L.vt[32 * w + 8 * g + x][(j & 32) + slot_of(j & 31)]);
+                const int row = 32 * w + 8 * g + x, at = (j & 32) + slot_of(j & 31);
+                const float v = widen(L.vt[row][piece_at(row, at >> 3) + (at & 7)]);
                 if (j <= i) V[x >> 2][x & 3] = fmaf(p, v, V[x >> 2][x & 3]);
               }
             }
@@ -320,7 +318,12 @@ __global__ __launch_bounds__(2 * D, 2) void linear_chunk_kernel(LinearArgs a, Li
           }
         }
       }
+    } else {
+      __syncthreads();
     }
+    // The next chunk's rows, which arrive during the update of the state.
+    fetch_kv(c + kChunk);
+    if (kAttend) fetch_q(c + kChunk, 0);
     __builtin_amdgcn_sched_barrier(0);
     const int g8 = again(8 * g);
     // S = l^n S + (l^(n-1-j) V's rows times K^T); rows from n on are zeros
@@ -339,35 +342,38 @@ __global__ __launch_bounds__(2 * D, 2) void linear_chunk_kernel(LinearArgs a, Li
       float d[8];
 #pragma unroll
       for (int b = 0; b < 8; ++b) d[b] = L.pw[max(n - 1 - (32 * s + (g8 >> 1) + (b & 3) + 4 * (b & 4)), 0)];
+      u32x4 vp[2][3];
 #pragma unroll
       for (int nt = 0; nt < 2; ++nt) {
-        const u32x4 vf = ld16(&L.vt[col + 4 * nt][32 * s + g8]);
-        u32x4 p0, p1, p2;
+        const u32x4 vf = ld16(&L.vt[col + 4 * nt][piece_at(col, 4 * s + (g8 >> 3))]);
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
           float x = low(vf[b]) * d[2 * b], y = high(vf[b]) * d[2 * b + 1];
-          p0[b] = part(x, y);
-          p1[b] = part(x, y);
-          p2[b] = pack2(x, y);
+          vp[nt][0][b] = part(x, y);
+          vp[nt][1][b] = part(x, y);
+          vp[nt][2][b] = pack2(x, y);
         }
+      }
+      // Four independent sums at a time: one product's result is the next but three's summand.
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-          const u32x4 kf = ld16(&L.kt[16 * mt + m][32 * s + g8]);
-          S[mt][nt] = mfma16(kf, p2, S[mt][nt]);
-          S[mt][nt] = mfma16(kf, p1, S[mt][nt]);
-          S[mt][nt] = mfma16(kf, p0, S[mt][nt]);
-        }
+      for (int mt = 0; mt < MT; mt += 2) {
+        const u32x4 kf[2] = {ld16(&L.kt[16 * mt + m][piece_at(16 * mt, 4 * s + (g8 >> 3))]),
+                             ld16(&L.kt[16 * mt + 16 + m][piece_at(16 * mt + 16, 4 * s + (g8 >> 3))])};
+#pragma unroll
+        for (int x = 2; x >= 0; --x)
+#pragma unroll
+          for (int y = 0; y < 4; ++y) S[mt + (y >> 1)][y & 1] = mfma16(kf[y >> 1], vp[y & 1][x], S[mt + (y >> 1)][y & 1]);
       }
     }
   }
   if (it.dst == -1) return;
-  float* to = state_at(a, it.dst, h, D);
+  float* to = state_at(a, it.dst, h, D) + 4 * g * D + col;
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
     for (int nt = 0; nt < 2; ++nt)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) to[(16 * mt + 4 * g + r) * D + col + 4 * nt] = S[mt][nt][r];
+      for (int r = 0; r < 4; ++r) to[(16 * mt + r) * D + 4 * nt] = S[mt][nt][r];
 }
 
 template <int D, class List>
