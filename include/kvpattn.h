@@ -333,10 +333,13 @@ int kv_append_rope(kvp_pool_t pool, int layer, const kvp_rope* rope, const void*
  * ------------------------------------------------------------------------------------------------- */
 #define KVP_LINEAR_MAX_HEADS 128
 
+/* Workspace bytes linear_chunk_attn needs (0 where no sequence is long enough to be cut into parts). */
+int linear_chunk_workspace_size(const int32_t* cu, int num_seqs, int num_kv_heads, int head_dim, size_t* bytes);
+
 /* Chunks: sequence i's tokens are the rows cu[i] .. cu[i+1] (none: its state is handed on as it is).
  *   cu  host int32 [num_seqs + 1], non-decreasing, cu[0] = 0
- * The strides are head_dim .. 2^24. */
-int linear_chunk_workspace_size(const int32_t* cu, int num_seqs, int num_kv_heads, int head_dim, size_t* bytes);
+ *   ws  device workspace of ws_bytes >= linear_chunk_workspace_size(...), 16-byte aligned
+ * The strides are head_dim .. 2^24.  Errors: KVP_EWORKSPACE if ws is too small. */
 int linear_chunk_attn(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
                       float* state, int num_slots, const float* decay, const int32_t* src_slots,
                       const int32_t* dst_slots, const int32_t* cu, int num_seqs, int num_q_heads, int num_kv_heads,

@@ -614,6 +614,41 @@ int check_cu(const int32_t* cu, int num_seqs) {
   return KVP_OK;
 }
 
+// The work of linear_chunk_attn.  Workgroups fit the GPU two to a compute unit; a sequence of more than twice an even
+// share of the call's tokens is cut into parts of about that share.
+struct LinearPlan {
+  std::vector<kvp::LinearItem> items, sums;
+  std::vector<kvp::LinearScan> scans;
+  int parts = 0;
+};
+constexpr int kLinearBlocks = 512, kLinearMinPart = 256, kLinearPartStep = 64;
+
+// src, dst: nullable (only the number of parts is wanted).
+void plan_linear(const int32_t* cu, int num_seqs, int num_kv_heads, const int32_t* src, const int32_t* dst,
+                 LinearPlan* P) {
+  const int64_t even = ((int64_t)cu[num_seqs] * num_kv_heads + kLinearBlocks - 1) / kLinearBlocks;
+  const int64_t share = std::max<int64_t>(kLinearMinPart, even);
+  for (int i = 0; i < num_seqs; ++i) {
+    const int32_t n = cu[i + 1] - cu[i], from = src ? src[i] : -1, to = dst ? dst[i] : -1;
+    if (n <= 2 * share) {
+      P->items.push_back({cu[i], n, from, to});
+      continue;
+    }
+    const int64_t want = (n + share - 1) / share;  // parts of a whole number of chunks
+    const int32_t len = (int32_t)(((n + want - 1) / want + kLinearPartStep - 1) / kLinearPartStep * kLinearPartStep);
+    const int32_t m = (n + len - 1) / len;
+    for (int32_t p = 0; p < m; ++p) {
+      const int32_t t0 = cu[i] + p * len, cnt = std::min(len, n - p * len);
+      P->items.push_back({t0, cnt, p == 0 && from < 0 ? -1 : -2 - (P->parts + p), p + 1 < m ? -1 : to});
+      if (p + 1 < m) P->sums.push_back({t0, cnt, -1, -2 - (P->parts + p + 1)});
+    }
+    P->scans.push_back({from, P->parts, m, len});
+    P->parts += m;
+  }
+  // longest first: the last workgroups to start are short
+  std::stable_sort(P->items.begin(), P->items.end(), [](const auto& x, const auto& y) { return x.n > y.n; });
+}
+
 constexpr int64_t kLinearMaxStride = 1 << 24;
 
 constexpr int32_t kRopeValid = 0x726f7065;  // kvp_rope.valid
@@ -989,11 +1024,21 @@ int kvp_rope_apply(const kvp_rope* rope, const void* x, int64_t x_token_stride, 
   return e == hipSuccess ? KVP_OK : hip_err(e, "kvp_rope_apply launch");
 }
 
-int linear_chunk_workspace_size(const int32_t* cu, int num_seqs, int num_kv_heads, int head_dim, size_t* bytes) {
+int linear_chunk_workspace_size(const int32_t* cu, int num_seqs, int num_kv_heads, int head_dim, size_t* bytes) try {
   if (!bytes) return set_err(KVP_EINVAL, "bytes is NULL");
   *bytes = 0;
   if (num_seqs < 0) return set_err(KVP_EINVAL, "num_seqs %d < 0", num_seqs);
-  return num_seqs == 0 ? KVP_OK : check_cu(cu, num_seqs);
+  if (num_kv_heads <= 0 || head_dim <= 0)
+    return set_err(KVP_EINVAL, "num_kv_heads %d or head_dim %d not positive", num_kv_heads, head_dim);
+  if (num_seqs == 0) return KVP_OK;
+  const int rc = check_cu(cu, num_seqs);
+  if (rc) return rc;
+  LinearPlan P;
+  plan_linear(cu, num_seqs, num_kv_heads, nullptr, nullptr, &P);
+  *bytes = (size_t)P.parts * num_kv_heads * head_dim * head_dim * sizeof(float);
+  return KVP_OK;
+} catch (const std::exception& x) {
+  return set_err(KVP_ENOMEM, "linear_chunk_workspace_size: %s", x.what());
 }
 
 int linear_chunk_attn(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
@@ -1011,22 +1056,34 @@ int linear_chunk_attn(const void* q, int64_t q_stride, const void* k, int64_t k_
   for (const int64_t stride : {q_stride, k_stride, v_stride})  // the kernel reads a chunk's rows at 32-bit offsets
     if (cu[num_seqs] > 0 && (stride < head_dim || stride > kLinearMaxStride))
       return set_err(KVP_EINVAL, "stride %lld outside [head_dim, %lld]", (long long)stride, (long long)kLinearMaxStride);
-  std::vector<kvp::LinearItem> items;
-  for (int i = 0; i < num_seqs; ++i) items.push_back({cu[i], cu[i + 1] - cu[i], src_slots[i], dst_slots[i]});
-  // longest first: the last workgroups to start are short
-  std::stable_sort(items.begin(), items.end(), [](const auto& x, const auto& y) { return x.n > y.n; });
-  const kvp::LinearArgs a = linear_args(q, q_stride, k, k_stride, v, v_stride, state, num_q_heads, num_kv_heads, scale,
-                                        out, out_dtype);
+  LinearPlan P;
+  plan_linear(cu, num_seqs, num_kv_heads, src_slots, dst_slots, &P);
+  const size_t need = (size_t)P.parts * num_kv_heads * head_dim * head_dim * sizeof(float);
+  if (need > 0 && (!ws || ws_bytes < need || (reinterpret_cast<uintptr_t>(ws) & 15) != 0))
+    return set_err(KVP_EWORKSPACE, "workspace of %zu bytes (16-byte aligned), %zu needed", ws ? ws_bytes : 0, need);
+  kvp::LinearArgs a = linear_args(q, q_stride, k, k_stride, v, v_stride, state, num_q_heads, num_kv_heads, scale, out,
+                                  out_dtype);
+  a.parts = reinterpret_cast<float*>(ws);
+  Packer meta;
+  const size_t off_items = meta.add(P.items.data(), P.items.size() * sizeof(kvp::LinearItem));
+  const size_t off_sums = meta.add(P.sums.data(), P.sums.size() * sizeof(kvp::LinearItem));
+  const size_t off_scans = meta.add(P.scans.data(), P.scans.size() * sizeof(kvp::LinearScan));
+  const size_t off_decay = meta.add(decay, num_kv_heads * sizeof(float));
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-  const size_t nb = items.size() * sizeof(kvp::LinearItem);
   Staging::Lease lease;
-  rc = staging().lease(nb + num_kv_heads * sizeof(float), s, &lease);
+  rc = staging().lease(meta.buf.size(), s, &lease);
   if (rc) return rc;
-  unsigned char* host = reinterpret_cast<unsigned char*>(lease.host);
-  std::memcpy(host, items.data(), nb);
-  std::memcpy(host + nb, decay, num_kv_heads * sizeof(float));
-  const kvp::LinearItems list{reinterpret_cast<const kvp::LinearItem*>(host), reinterpret_cast<const float*>(host + nb)};
-  const hipError_t e = kvp::launch_linear_chunk(a, list, (int)items.size(), head_dim, s);
+  std::memcpy(lease.host, meta.buf.data(), meta.buf.size());
+  const unsigned char* host = reinterpret_cast<const unsigned char*>(lease.host);
+  kvp::LinearItems list{};
+  list.items = reinterpret_cast<const kvp::LinearItem*>(host + off_items);
+  list.sums = reinterpret_cast<const kvp::LinearItem*>(host + off_sums);
+  list.scans = reinterpret_cast<const kvp::LinearScan*>(host + off_scans);
+  list.decay = reinterpret_cast<const float*>(host + off_decay);
+  list.n_items = (int)P.items.size();
+  list.n_sums = (int)P.sums.size();
+  list.n_scans = (int)P.scans.size();
+  const hipError_t e = kvp::launch_linear_chunk(a, list, head_dim, s);
   const int rr = staging().release(lease, e == hipSuccess);
   return e == hipSuccess ? rr : hip_err(e, "linear_chunk_attn launch");
 } catch (const std::exception& x) {

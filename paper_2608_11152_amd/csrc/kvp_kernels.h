@@ -73,10 +73,18 @@ struct LinearList {
   float decay[kLinearHeads];
 };
 
-// The same in pinned host memory (linear_chunk_attn).
+// A sequence cut into n parts of len tokens (the last may be shorter): slots part .. part + n - 1 of the workspace.
+struct LinearScan {
+  int32_t src, part, n, len;
+};
+
+// linear_chunk_attn: the same in pinned host memory.  Slots below -1 are parts of long sequences, -2 the first.
 struct LinearItems {
   const LinearItem* items;
+  const LinearItem* sums;   // parts whose sums are needed
+  const LinearScan* scans;
   const float* decay;
+  int n_items, n_sums, n_scans;
 };
 
 struct LinearArgs {
@@ -223,7 +231,7 @@ hipError_t launch_append(const AppendArgs& a, int D, hipStream_t s);
 hipError_t launch_append_rope(const AppendRopeArgs& a, int D, hipStream_t s);
 hipError_t launch_rope(const RopeArgs& a, bool f32, hipStream_t s);
 hipError_t launch_linear_decode(const LinearArgs& a, const LinearList& list, int n_items, int D, hipStream_t s);
-hipError_t launch_linear_chunk(const LinearArgs& a, const LinearItems& list, int n_items, int D, hipStream_t s);
+hipError_t launch_linear_chunk(const LinearArgs& a, const LinearItems& list, int D, hipStream_t s);
 hipError_t launch_gather(const GatherArgs& a, int D, hipStream_t s);
 hipError_t launch_fill_zero(void* p, size_t bytes, hipStream_t s);
 // Copy n bytes from pinned host memory (src) to device memory (dst; 16-byte aligned, like src) with a

@@ -17,6 +17,10 @@
 // dims of Q and K and the tokens of K^T and V^T lie in that order in LDS, and the state and the weights of a chunk go
 // from one product's result into the next one's operand without leaving their registers:
 //   P^T (keys x rows)   = K Q^T           O^T (columns x rows) = S^T Q^T + V^T P^T           S (dims x columns) = K^T V
+// A sequence that would leave compute units without work is cut into parts (plan_linear): linear_chunk_kernel without its
+// outputs sums each part from zeros, linear_scan_kernel turns the sums into the states before the parts, and the parts are
+// items.  The parts' keys and values are read twice.
+//
 // Each wave computes all of P^T (a tenth of its matrix work) rather than share it through LDS and a barrier.
 //
 // Operands that are not bf16 are carried as sums of bf16 parts: S and P as two (2^-18 left: far inside a bf16 output's
@@ -376,6 +380,35 @@ __global__ __launch_bounds__(2 * D, 2) void linear_chunk_kernel(LinearArgs a, Li
       for (int r = 0; r < 4; ++r) to[(16 * mt + r) * D + 4 * nt] = S[mt][nt][r];
 }
 
+// States before each part of the long sequences, from the parts' own sums: S_0 = source, S_i = l^len S_(i-1) + sum_(i-1).
+// Slot i of a sequence's parts holds sum_(i-1) before and S_i afterwards.  One thread per element, in 64 bits: the decay
+// of one part meets that of hundreds.
+__global__ __launch_bounds__(256) void linear_scan_kernel(LinearArgs a, LinearItems list, int D) {
+  const int per = D * D / 256, e = (blockIdx.x % per) * 256 + threadIdx.x;
+  const int h = blockIdx.x / per % a.Hkv;
+  const LinearScan sc = list.scans[blockIdx.x / per / a.Hkv];
+  const double f = power((double)list.decay[h], sc.len);
+  float* p = state_at(a, -2 - sc.part, h, D) + e;
+  const int64_t step = (int64_t)a.Hkv * D * D;
+  double S = 0.0;
+  if (sc.src >= 0) {
+    const float x = state_at(a, sc.src, h, D)[e];
+    p[0] = x;
+    S = x;
+  }
+  constexpr int U = 16;  // loads in flight
+  for (int i = 1; i < sc.n; i += U) {
+    float x[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) x[u] = i + u < sc.n ? p[(i + u) * step] : 0.0f;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      S = fma(S, f, (double)x[u]);
+      if (i + u < sc.n) p[(i + u) * step] = (float)S;
+    }
+  }
+}
+
 template <int D, class List>
 __global__ __launch_bounds__(D) void linear_step_kernel(LinearArgs a, List list) {
   __shared__ float ks[D], qs[16][D];
@@ -420,11 +453,21 @@ hipError_t launch_linear_decode(const LinearArgs& a, const LinearList& list, int
   return hipGetLastError();
 }
 
-hipError_t launch_linear_chunk(const LinearArgs& a, const LinearItems& list, int n_items, int D, hipStream_t s) {
-  if (n_items == 0) return hipSuccess;
-  const dim3 grid(n_items * a.Hkv);
-  if (D == 128) hipLaunchKernelGGL((linear_chunk_kernel<128, true>), grid, dim3(256), 0, s, a, list);
-  else hipLaunchKernelGGL((linear_chunk_kernel<64, true>), grid, dim3(128), 0, s, a, list);
+template <int D>
+static void launch_chunk(const LinearArgs& a, const LinearItems& list, hipStream_t s) {
+  if (list.n_scans > 0) {
+    LinearItems sums = list;
+    sums.items = list.sums;
+    hipLaunchKernelGGL((linear_chunk_kernel<D, false>), dim3(list.n_sums * a.Hkv), dim3(2 * D), 0, s, a, sums);
+    hipLaunchKernelGGL(linear_scan_kernel, dim3(list.n_scans * a.Hkv * (D * D / 256)), dim3(256), 0, s, a, list, D);
+  }
+  hipLaunchKernelGGL((linear_chunk_kernel<D, true>), dim3(list.n_items * a.Hkv), dim3(2 * D), 0, s, a, list);
+}
+
+hipError_t launch_linear_chunk(const LinearArgs& a, const LinearItems& list, int D, hipStream_t s) {
+  if (list.n_items == 0) return hipSuccess;
+  if (D == 128) launch_chunk<128>(a, list, s);
+  else launch_chunk<64>(a, list, s);
   return hipGetLastError();
 }
 
