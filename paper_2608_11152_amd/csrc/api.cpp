@@ -649,6 +649,8 @@ void plan_linear(const int32_t* cu, int num_seqs, int num_kv_heads, const int32_
   std::stable_sort(P->items.begin(), P->items.end(), [](const auto& x, const auto& y) { return x.n > y.n; });
 }
 
+static_assert(kvp::kLinearHeads == KVP_LINEAR_MAX_HEADS && kvp::kRopePairs == KVP_ROPE_PAIRS, "as in the header");
+
 constexpr int64_t kLinearMaxStride = 1 << 24;
 
 constexpr int32_t kRopeValid = 0x726f7065;  // kvp_rope.valid
@@ -1101,13 +1103,14 @@ int linear_decode_attn(const void* q, int64_t q_stride, const void* k, int64_t k
   if (rc) return rc;
   const kvp::LinearArgs a = linear_args(q, q_stride, k, k_stride, v, v_stride, state, num_q_heads, num_kv_heads, scale,
                                         out, out_dtype);
-  kvp::LinearList list{};
-  std::memcpy(list.decay, decay, sizeof(float) * num_kv_heads);
+  kvp::LinearBatch batch;
+  std::memcpy(batch.decay, decay, sizeof(float) * num_kv_heads);
   hipError_t e = hipSuccess;
   for (int i = 0; i < num_seqs && e == hipSuccess; i += kvp::kLinearBatch) {
     const int n = std::min(kvp::kLinearBatch, num_seqs - i);
-    for (int j = 0; j < n; ++j) list.items[j] = {i + j, 1, src_slots[i + j], dst_slots[i + j]};
-    e = kvp::launch_linear_decode(a, list, n, head_dim, reinterpret_cast<hipStream_t>(stream));
+    for (int j = 0; j < n; ++j) batch.slots[j] = make_int2(src_slots[i + j], dst_slots[i + j]);
+    batch.first = i;
+    e = kvp::launch_linear_decode(a, batch, n, head_dim, reinterpret_cast<hipStream_t>(stream));
   }
   return e == hipSuccess ? KVP_OK : hip_err(e, "linear_decode_attn launch");
 } catch (const std::exception& x) {

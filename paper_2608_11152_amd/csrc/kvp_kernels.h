@@ -66,11 +66,13 @@ struct LinearItem {
   int32_t src, dst;         // state slots; -1: starts from zeros / is not kept
 };
 
-// Items and decay rates travel in the launch arguments (linear_decode_attn reads no host memory later).
-constexpr int kLinearBatch = 192, kLinearHeads = 128;
-struct LinearList {
-  LinearItem items[kLinearBatch];
+// linear_decode_attn: slots (source, destination) of up to kLinearBatch sequences and the heads' decay, in the launch
+// arguments (4 KB at most), so that no host memory is read later.
+constexpr int kLinearBatch = 320, kLinearHeads = 128;
+struct LinearBatch {
+  int2 slots[kLinearBatch];
   float decay[kLinearHeads];
+  int32_t first;            // token of slots[0]
 };
 
 // A sequence cut into n parts of len tokens (the last may be shorter): slots part .. part + n - 1 of the workspace.
@@ -78,7 +80,7 @@ struct LinearScan {
   int32_t src, part, n, len;
 };
 
-// linear_chunk_attn: the same in pinned host memory.  Slots below -1 are parts of long sequences, -2 the first.
+// linear_chunk_attn: its work, in pinned host memory.  Slots below -1 are parts of long sequences, -2 the first.
 struct LinearItems {
   const LinearItem* items;
   const LinearItem* sums;   // parts whose sums are needed
@@ -230,7 +232,7 @@ struct TableArgs {
 hipError_t launch_append(const AppendArgs& a, int D, hipStream_t s);
 hipError_t launch_append_rope(const AppendRopeArgs& a, int D, hipStream_t s);
 hipError_t launch_rope(const RopeArgs& a, bool f32, hipStream_t s);
-hipError_t launch_linear_decode(const LinearArgs& a, const LinearList& list, int n_items, int D, hipStream_t s);
+hipError_t launch_linear_decode(const LinearArgs& a, const LinearBatch& batch, int n, int D, hipStream_t s);
 hipError_t launch_linear_chunk(const LinearArgs& a, const LinearItems& list, int D, hipStream_t s);
 hipError_t launch_gather(const GatherArgs& a, int D, hipStream_t s);
 hipError_t launch_fill_zero(void* p, size_t bytes, hipStream_t s);

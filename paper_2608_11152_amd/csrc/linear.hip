@@ -2,8 +2,7 @@
 //   S_t = decay S_{t-1} + k_t v_t^T,   o_t = scale q_t^T S_t
 // q, k, v bf16, the state and every sum fp32; the output is rounded once.
 //
-// linear_step_kernel: the recurrence itself for single tokens: one workgroup per (sequence, KV head), thread c holds
-// column c of the state in registers.
+// linear_token_kernel: single tokens.
 //
 // linear_chunk_kernel: chunks of 64 tokens, from the state S before the chunk (rows i, j of the chunk, l = decay):
 //   O = (l^(i+1) Q) S + (Q K^T . l^(i-j) for j <= i) V          S' = l^64 S + (l^(63-j) K)^T V
@@ -409,47 +408,71 @@ __global__ __launch_bounds__(256) void linear_scan_kernel(LinearArgs a, LinearIt
   }
 }
 
-template <int D, class List>
-__global__ __launch_bounds__(D) void linear_step_kernel(LinearArgs a, List list) {
-  __shared__ float ks[D], qs[16][D];
-  const LinearItem it = list.items[blockIdx.x];
-  const int h = blockIdx.y, c = threadIdx.x, G = a.Hq / a.Hkv;
-  const float decay = list.decay[h];
-  float S[D];
-  const float* from = a.state + ((int64_t)it.src * a.Hkv + h) * D * D + c;
+// Single tokens: one workgroup per (sequence, KV head).  A thread holds 4 columns of D / R rows of the state, R apart, all
+// loads issued before the first is used; the rows' sums for the output meet in the wave and then in LDS.  Bandwidth is
+// what bounds it: the state is read and written once, past the caches.
+template <int D>
+__global__ __launch_bounds__(256) void linear_token_kernel(LinearArgs a, LinearBatch batch) {
+  constexpr int C = D / 4, R = 256 / C, N = D / R;  // threads per row, rows at a time, rows per thread
+  __shared__ float ks[D], qs[16][D], part[4][16][D];
+  const int tid = threadIdx.x, w = tid >> 6, c = 4 * (tid % C), r0 = tid / C;
+  const int i = blockIdx.x / a.Hkv, h = blockIdx.x - i * a.Hkv, G = a.Hq / a.Hkv;
+  const int src = batch.slots[i].x, dst = batch.slots[i].y;
+  const int64_t t = batch.first + i;
+  f32x4 S[N] = {};
+  if (src >= 0) {
+    const float* from = state_at(a, src, h, D) + r0 * D + c;
 #pragma unroll
-  for (int r = 0; r < D; ++r) S[r] = it.src >= 0 ? from[r * D] : 0.0f;
-  for (int i = 0; i < it.n; ++i) {
-    const int64_t t = (int64_t)it.t0 + i;
-    __syncthreads();
-    ks[c] = widen(a.k[t * a.k_stride + h * D + c]);
-    for (int g = 0; g < G; ++g) qs[g][c] = widen(a.q[t * a.q_stride + (h * G + g) * D + c]);
-    const float v = widen(a.v[t * a.v_stride + h * D + c]);
-    __syncthreads();
-#pragma unroll
-    for (int r = 0; r < D; ++r) S[r] = fmaf(ks[r], v, decay * S[r]);
-    for (int g = 0; g < G; ++g) {
-      float o = 0.0f;
-#pragma unroll
-      for (int r = 0; r < D; ++r) o = fmaf(qs[g][r], S[r], o);
-      const int64_t at = (t * a.Hq + h * G + g) * D + c;
-      if (a.out_f32) reinterpret_cast<float*>(a.out)[at] = o * a.scale;
-      else reinterpret_cast<uint16_t*>(a.out)[at] = narrow(o * a.scale);
-    }
+    for (int n = 0; n < N; ++n) S[n] = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(from + n * R * D));
   }
-  if (it.dst < 0) return;
-  float* to = a.state + ((int64_t)it.dst * a.Hkv + h) * D * D + c;
+  if (tid < D) ks[tid] = widen(a.k[t * a.k_stride + h * D + tid]);
+  for (int e = tid; e < G * D; e += 256) qs[e / D][e % D] = widen(a.q[t * a.q_stride + h * G * D + e]);
+  const u32x2 vw = *reinterpret_cast<const u32x2*>(a.v + t * a.v_stride + h * D + c);
+  const f32x4 v{low(vw[0]), high(vw[0]), low(vw[1]), high(vw[1])};
+  const float decay = batch.decay[h];
+  __syncthreads();
 #pragma unroll
-  for (int r = 0; r < D; ++r) to[r * D] = S[r];
+  for (int n = 0; n < N; ++n) {
+    const float k = ks[r0 + n * R];
+#pragma unroll
+    for (int x = 0; x < 4; ++x) S[n][x] = fmaf(k, v[x], decay * S[n][x]);
+  }
+  if (dst >= 0) {
+    float* to = state_at(a, dst, h, D) + r0 * D + c;
+#pragma unroll
+    for (int n = 0; n < N; ++n) __builtin_nontemporal_store(S[n], reinterpret_cast<f32x4*>(to + n * R * D));
+  }
+  for (int g = 0; g < G; ++g) {
+    f32x4 o = {};
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const float q = qs[g][r0 + n * R];
+#pragma unroll
+      for (int x = 0; x < 4; ++x) o[x] = fmaf(q, S[n][x], o[x]);
+    }
+#pragma unroll
+    for (int d = C; d < 64; d *= 2)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) o[x] += __shfl_xor(o[x], d);
+    if ((tid & 63) < C) *reinterpret_cast<f32x4*>(&part[w][g][c]) = o;
+  }
+  __syncthreads();
+  for (int e = tid; e < G * D; e += 256) {
+    const int g = e / D, x = e % D;
+    const float o = a.scale * (part[0][g][x] + part[1][g][x] + (part[2][g][x] + part[3][g][x]));
+    const int64_t at = (t * a.Hq + h * G) * D + e;
+    if (a.out_f32) reinterpret_cast<float*>(a.out)[at] = o;
+    else reinterpret_cast<uint16_t*>(a.out)[at] = narrow(o);
+  }
 }
 
 }  // namespace
 
-hipError_t launch_linear_decode(const LinearArgs& a, const LinearList& list, int n_items, int D, hipStream_t s) {
-  if (n_items == 0) return hipSuccess;
-  const dim3 grid(n_items, a.Hkv);
-  if (D == 128) hipLaunchKernelGGL((linear_step_kernel<128, LinearList>), grid, dim3(128), 0, s, a, list);
-  else hipLaunchKernelGGL((linear_step_kernel<64, LinearList>), grid, dim3(64), 0, s, a, list);
+hipError_t launch_linear_decode(const LinearArgs& a, const LinearBatch& batch, int n, int D, hipStream_t s) {
+  if (n == 0) return hipSuccess;
+  const dim3 grid(n * a.Hkv);
+  if (D == 128) hipLaunchKernelGGL(linear_token_kernel<128>, grid, dim3(256), 0, s, a, batch);
+  else hipLaunchKernelGGL(linear_token_kernel<64>, grid, dim3(256), 0, s, a, batch);
   return hipGetLastError();
 }
 
