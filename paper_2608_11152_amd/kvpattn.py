@@ -98,14 +98,14 @@ def lib() -> C.CDLL:
         L.kvp_prefix_table_error.argtypes = [p, C.POINTER(i)]
         L.kvp_check_tables.argtypes = [i32p, i, i32p, i, i, gpp]
         L.kvp_plan_decode.argtypes = [i32p, i, gpp, i, i, i32p, i, C.POINTER(i), C.POINTER(i), C.POINTER(i)]
-        rp, f32p, i64, dbl = C.POINTER(RopeStruct), C.POINTER(C.c_float), C.c_int64, C.c_double
+        rp, i64, dbl = C.POINTER(RopeStruct), C.c_int64, C.c_double
         L.kvp_rope_init.argtypes = [rp, i, i, dbl, dbl, i, dbl, dbl, dbl]
         L.kvp_rope_apply.argtypes = [rp, vp, i64, i64, vp, i64, i64, i, vp, i64, i, i, i, vp]
-        L.kv_append_rope.argtypes = [p, i, rp, vp, i64, vp, i64, vp, i64, vp, i64, i, vp, i, i32p, i32p, i, gpp, vp]
-        L.linear_chunk_workspace_size.argtypes = [i32p, i, i, i, C.POINTER(sz)]
-        L.linear_chunk_attn.argtypes = [vp, i64, vp, i64, vp, i64, vp, i, f32p, i32p, i32p, i32p, i, i, i, i, C.c_float,
+        L.kv_append_rope.argtypes = [p, i, rp, vp, i64, vp, i64, vp, i64, vp, i64, i, vp, i, vp, vp, i, gpp, vp]
+        L.linear_chunk_workspace_size.argtypes = [vp, i, i, i, C.POINTER(sz)]
+        L.linear_chunk_attn.argtypes = [vp, i64, vp, i64, vp, i64, vp, i, vp, vp, vp, vp, i, i, i, i, C.c_float,
                                         vp, i, vp, sz, vp]
-        L.linear_decode_attn.argtypes = [vp, i64, vp, i64, vp, i64, vp, i, f32p, i32p, i32p, i, i, i, i, C.c_float, vp, i,
+        L.linear_decode_attn.argtypes = [vp, i64, vp, i64, vp, i64, vp, i, vp, vp, vp, i, i, i, i, C.c_float, vp, i,
                                          vp]
         L.kvp_strerror.argtypes = [i]
         L.kvp_strerror.restype = C.c_char_p
@@ -156,9 +156,9 @@ def _gp_ref(gp):
 
 
 def _stream(stream):
-    if stream is None:
+    if stream is None:  # (torch.cuda.current_stream() makes an object of it first: 4 us of a 13 us call)
         import torch
-        return C.c_void_p(torch.cuda.current_stream().cuda_stream)
+        return C.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
     if isinstance(stream, int):
         return C.c_void_p(stream)
     return C.c_void_p(stream.cuda_stream)
@@ -218,33 +218,40 @@ def _dev(t, name: str, dtypes, ndim: int | None = None, rows: int | None = None,
     return t
 
 
-def _heads(t, name: str, dtypes, rows: int | None = None):
+def _heads(t, name: str, dtypes, rows: int = 0):
     """A [tokens, heads, head_dim] tensor whose heads may lie apart (rows of a fused projection, for instance) while
-    the elements of a head are dense, on the current device."""
+    the elements of a head are dense, on the current device.  Returns its shape and strides."""
     import torch
-    if not getattr(t, "is_cuda", False):
+    dev = t.get_device() if hasattr(t, "get_device") else -1
+    if dev < 0:
         raise ValueError(f"{name} must be a GPU tensor")
     if t.dtype not in dtypes:
         raise ValueError(f"{name} has dtype {t.dtype}; expected one of {', '.join(str(d) for d in dtypes)}")
-    if t.dim() != 3:
-        raise ValueError(f"{name} has {t.dim()} dimensions, expected 3")
-    if t.shape[2] > 1 and t.stride(2) != 1:
+    shape, st = t.shape, t.stride()
+    if len(shape) != 3:
+        raise ValueError(f"{name} has {len(shape)} dimensions, expected 3")
+    if st[2] != 1 and shape[2] > 1:
         raise ValueError(f"{name}'s head elements must be contiguous")
-    if rows is not None and t.shape[0] < rows:
-        raise ValueError(f"{name} has {t.shape[0]} rows, {rows} needed")
-    if t.device.index != torch.cuda.current_device():
-        raise ValueError(f"{name} is on device {t.device.index}, the current device is {torch.cuda.current_device()}")
-    return t
+    if shape[0] < rows:
+        raise ValueError(f"{name} has {shape[0]} rows, {rows} needed")
+    if dev != torch.cuda.current_device():
+        raise ValueError(f"{name} is on device {dev}, the current device is {torch.cuda.current_device()}")
+    return shape, st
 
 
 def _rows(t, name: str, rows: int, heads: int | None = None, d: int | None = None) -> int:
     """Checks a bf16 [tokens, heads, d] tensor whose tokens may lie apart; returns the stride between them."""
-    _heads(t, name, _bf16(), rows)
-    if (heads is not None and t.shape[1] != heads) or (d is not None and t.shape[2] != d):
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected (*, {heads}, {d})")
-    if t.shape[1] > 1 and t.stride(1) != t.shape[2]:
+    shape, st = _heads(t, name, _bf16(), rows)
+    if (heads is not None and shape[1] != heads) or (d is not None and shape[2] != d):
+        raise ValueError(f"{name} has shape {tuple(shape)}, expected (*, {heads}, {d})")
+    if st[1] != shape[2] and shape[1] > 1:
         raise ValueError(f"{name}'s heads must be contiguous")
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+    return st[0] if shape[0] > 1 else shape[1] * shape[2]
+
+
+def _addr(a: np.ndarray) -> int:
+    """Address of a host array, for arguments declared as bare pointers (a typed ctypes pointer takes 2 us to make)."""
+    return a.__array_interface__["data"][0]
 
 
 def _bf16():
@@ -368,8 +375,10 @@ class Rope:
                                    high_turns, magnitude), "kvp_rope_init")
         self.rotary_dim = rotary_dim
 
+        self._ref = C.byref(self.s)
+
     def ref(self):
-        return C.byref(self.s)
+        return self._ref
 
 
 def kvp_rope_apply(rope: Rope, x, positions, out=None, grad: bool = False, stream=None):
@@ -377,19 +386,18 @@ def kvp_rope_apply(rope: Rope, x, positions, out=None, grad: bool = False, strea
     grad: the transpose, for the gradient.  `out` may be x; a new tensor is dense."""
     import torch
     dtypes = (torch.bfloat16, torch.float32)
-    _heads(x, "x", dtypes)
-    T, H, d = x.shape
+    (T, H, d), xs = _heads(x, "x", dtypes)
     _dev(positions, "positions", _i32t(), 1, rows=T)
-    if positions.device != x.device:
+    if positions.get_device() != x.get_device():
         raise ValueError(f"positions is on {positions.device}, x on {x.device}")
     if out is None:
-        out = _alloc_on(stream, (T, H, d), x.dtype, x.device)
+        out, ys = _alloc_on(stream, (T, H, d), x.dtype, x.device), (H * d, d)
     else:
-        _heads(out, "out", (x.dtype,))
-        if out.shape != x.shape:
-            raise ValueError(f"out has shape {tuple(out.shape)}, x {tuple(x.shape)}")
-    _check(lib().kvp_rope_apply(rope.ref(), _dptr(x), x.stride(0), x.stride(1), _dptr(out), out.stride(0), out.stride(1),
-                                KVP_F32 if x.dtype == torch.float32 else KVP_BF16, _dptr(positions), T, H, d, int(grad),
+        shape, ys = _heads(out, "out", (x.dtype,))
+        if shape != x.shape:
+            raise ValueError(f"out has shape {tuple(shape)}, x {tuple(x.shape)}")
+    _check(lib().kvp_rope_apply(rope.ref(), x.data_ptr(), xs[0], xs[1], out.data_ptr(), ys[0], ys[1],
+                                KVP_F32 if x.dtype == torch.float32 else KVP_BF16, positions.data_ptr(), T, H, d, int(grad),
                                 _stream(stream)), "kvp_rope_apply")
     return out
 
@@ -410,12 +418,14 @@ def kv_append_rope(pool: Pool, layer, rope: Rope, k, v, block_tables, start_pos,
         Hq = q.shape[1] if q.dim() == 3 else 0
         qs = _rows(q, "q", T, Hq, pool.head_dim)
         if q_out is None:
-            q_out = _alloc_on(stream, tuple(q.shape), q.dtype, q.device)
-        os_ = _rows(q_out, "q_out", T, Hq, pool.head_dim)
+            q_out, os_ = _alloc_on(stream, q.shape, q.dtype, q.device), Hq * pool.head_dim
+        else:
+            os_ = _rows(q_out, "q_out", T, Hq, pool.head_dim)
     elif q_out is not None:
         raise ValueError("q_out without q")
-    _check(lib().kv_append_rope(pool.handle, layer, rope.ref(), _dptr(k), ks, _dptr(v), vs, _dptr(q), qs, _dptr(q_out),
-                                os_, Hq, _dptr(block_tables), block_tables.shape[1], _ptr(sp), _ptr(cu), len(sp),
+    _check(lib().kv_append_rope(pool.handle, layer, rope.ref(), k.data_ptr(), ks, v.data_ptr(), vs,
+                                None if q is None else q.data_ptr(), qs, None if q is None else q_out.data_ptr(), os_, Hq,
+                                block_tables.data_ptr(), block_tables.shape[1], _addr(sp), _addr(cu), len(sp),
                                 _gp_ref(group_prefix), _stream(stream)), "kv_append_rope")
     return q_out
 
@@ -429,7 +439,7 @@ def _linear_args(q, k, v, state, decay, src_slots, dst_slots, rows, scale, out, 
         raise ValueError(f"src_slots has shape {src.shape}, dst_slots {dst.shape}: one slot per sequence each")
     qs = _rows(q, "q", rows)
     T, Hq, d = q.shape
-    ks = _rows(k, "k", rows, d=d, heads=k.shape[1] if k.dim() == 3 else None)
+    ks = _rows(k, "k", rows, None, d)
     Hkv = k.shape[1]
     vs = _rows(v, "v", rows, Hkv, d)
     if dec.shape != (Hkv,):
@@ -438,20 +448,20 @@ def _linear_args(q, k, v, state, decay, src_slots, dst_slots, rows, scale, out, 
     if out is None:
         out = _alloc_on(stream, (T, Hq, d), out_dtype or torch.float32, q.device)
     _dev(out, "out", _outt(), 3, rows=rows, tail=(Hq, d))
-    if state.device != q.device or out.device != q.device:
+    if not state.get_device() == out.get_device() == q.get_device():
         raise ValueError(f"q is on {q.device}, state on {state.device}, out on {out.device}")
     if scale is None:
         scale = 1.0 / math.sqrt(d)
-    head = (_dptr(q), qs, _dptr(k), ks, _dptr(v), vs, _dptr(state), state.shape[0],
-            dec.ctypes.data_as(C.POINTER(C.c_float)), _ptr(src), _ptr(dst))
-    tail = (len(src), Hq, Hkv, d, float(scale), _dptr(out), KVP_F32 if out.dtype == torch.float32 else KVP_BF16)
+    head = (q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs, state.data_ptr(), state.shape[0], _addr(dec), _addr(src),
+            _addr(dst))
+    tail = (len(src), Hq, Hkv, d, float(scale), out.data_ptr(), KVP_F32 if out.dtype == torch.float32 else KVP_BF16)
     return head, tail, out, (dec, src, dst)
 
 
 def linear_chunk_workspace_size(cu, num_kv_heads: int, head_dim: int) -> int:
     cu = _i32(cu)
     n = C.c_size_t()
-    _check(lib().linear_chunk_workspace_size(_ptr(cu), len(cu) - 1, num_kv_heads, head_dim, C.byref(n)),
+    _check(lib().linear_chunk_workspace_size(_addr(cu), len(cu) - 1, num_kv_heads, head_dim, C.byref(n)),
            "linear_chunk_workspace_size")
     return n.value
 
@@ -467,9 +477,12 @@ def linear_chunk_attn(q, k, v, state, decay, src_slots, dst_slots, cu, scale=Non
     head, tail, out, keep = _linear_args(q, k, v, state, decay, src_slots, dst_slots, int(cu[-1]), scale, out, out_dtype,
                                          stream)
     if ws is None:
-        ws = _alloc_on(stream, max(1, linear_chunk_workspace_size(cu, k.shape[1], k.shape[2])), torch.uint8, q.device)
-    _dev(ws, "ws", (ws.dtype,))
-    _check(lib().linear_chunk_attn(*head, _ptr(cu), *tail, _dptr(ws), ws.numel() * ws.element_size(), _stream(stream)),
+        n = linear_chunk_workspace_size(cu, k.shape[1], k.shape[2])
+        ws = _alloc_on(stream, n, torch.uint8, q.device) if n else None
+    else:
+        _dev(ws, "ws", (ws.dtype,))
+    _check(lib().linear_chunk_attn(*head, _addr(cu), *tail, None if ws is None else ws.data_ptr(),
+                                   0 if ws is None else ws.numel() * ws.element_size(), _stream(stream)),
            "linear_chunk_attn")
     return out
 
