@@ -414,9 +414,12 @@ __global__ __launch_bounds__(256) void linear_scan_kernel(LinearArgs a, LinearIt
 template <int D>
 __global__ __launch_bounds__(256) void linear_token_kernel(LinearArgs a, LinearBatch batch) {
   constexpr int C = D / 4, R = 256 / C, N = D / R;  // threads per row, rows at a time, rows per thread
-  __shared__ float ks[D], qs[16][D], part[4][16][D];
+  extern __shared__ float lds[];  // k, then per query head q and the waves' sums: (1 + 5 G) D
+  float* const ks = lds;
+  float* const qs = ks + D;
   const int tid = threadIdx.x, w = tid >> 6, c = 4 * (tid % C), r0 = tid / C;
   const int i = blockIdx.x / a.Hkv, h = blockIdx.x - i * a.Hkv, G = a.Hq / a.Hkv;
+  float* const part = qs + G * D;  // [G][4][D]
   const int src = batch.slots[i].x, dst = batch.slots[i].y;
   const int64_t t = batch.first + i;
   f32x4 S[N] = {};
@@ -426,7 +429,7 @@ __global__ __launch_bounds__(256) void linear_token_kernel(LinearArgs a, LinearB
     for (int n = 0; n < N; ++n) S[n] = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(from + n * R * D));
   }
   if (tid < D) ks[tid] = widen(a.k[t * a.k_stride + h * D + tid]);
-  for (int e = tid; e < G * D; e += 256) qs[e / D][e % D] = widen(a.q[t * a.q_stride + h * G * D + e]);
+  for (int e = tid; e < G * D; e += 256) qs[e] = widen(a.q[t * a.q_stride + h * G * D + e]);
   const u32x2 vw = *reinterpret_cast<const u32x2*>(a.v + t * a.v_stride + h * D + c);
   const f32x4 v{low(vw[0]), high(vw[0]), low(vw[1]), high(vw[1])};
   const float decay = batch.decay[h];
@@ -446,7 +449,7 @@ __global__ __launch_bounds__(256) void linear_token_kernel(LinearArgs a, LinearB
     f32x4 o = {};
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-      const float q = qs[g][r0 + n * R];
+      const float q = qs[g * D + r0 + n * R];
 #pragma unroll
       for (int x = 0; x < 4; ++x) o[x] = fmaf(q, S[n][x], o[x]);
     }
@@ -454,12 +457,12 @@ __global__ __launch_bounds__(256) void linear_token_kernel(LinearArgs a, LinearB
     for (int d = C; d < 64; d *= 2)
 #pragma unroll
       for (int x = 0; x < 4; ++x) o[x] += __shfl_xor(o[x], d);
-    if ((tid & 63) < C) *reinterpret_cast<f32x4*>(&part[w][g][c]) = o;
+    if ((tid & 63) < C) *reinterpret_cast<f32x4*>(part + (4 * g + w) * D + c) = o;
   }
   __syncthreads();
   for (int e = tid; e < G * D; e += 256) {
-    const int g = e / D, x = e % D;
-    const float o = a.scale * (part[0][g][x] + part[1][g][x] + (part[2][g][x] + part[3][g][x]));
+    const float* p = part + 4 * (e / D) * D + e % D;
+    const float o = a.scale * (p[0] + p[D] + (p[2 * D] + p[3 * D]));
     const int64_t at = (t * a.Hq + h * G) * D + e;
     if (a.out_f32) reinterpret_cast<float*>(a.out)[at] = o;
     else reinterpret_cast<uint16_t*>(a.out)[at] = narrow(o);
@@ -471,8 +474,9 @@ __global__ __launch_bounds__(256) void linear_token_kernel(LinearArgs a, LinearB
 hipError_t launch_linear_decode(const LinearArgs& a, const LinearBatch& batch, int n, int D, hipStream_t s) {
   if (n == 0) return hipSuccess;
   const dim3 grid(n * a.Hkv);
-  if (D == 128) hipLaunchKernelGGL(linear_token_kernel<128>, grid, dim3(256), 0, s, a, batch);
-  else hipLaunchKernelGGL(linear_token_kernel<64>, grid, dim3(256), 0, s, a, batch);
+  const size_t lds = (size_t)(1 + 5 * (a.Hq / a.Hkv)) * D * sizeof(float);
+  if (D == 128) hipLaunchKernelGGL(linear_token_kernel<128>, grid, dim3(256), lds, s, a, batch);
+  else hipLaunchKernelGGL(linear_token_kernel<64>, grid, dim3(256), lds, s, a, batch);
   return hipGetLastError();
 }
 
