@@ -31,6 +31,22 @@ struct AppendArgs {
   float inv_scale_k, inv_scale_v;
 };
 
+// n / d for n < 2^31: with 2^(s-1) < d <= 2^s and mul = ceil(2^(31+s) / d), mul d exceeds 2^(31+s) by less than
+// d <= 2^s, so n mul / 2^(31+s) exceeds n / d by less than 1 / d.
+struct FastDiv {
+  uint32_t d = 1, mul = 0, shift = 0;
+  FastDiv() = default;
+  explicit FastDiv(uint32_t div) : d(div) {
+    uint32_t s = 0;
+    while ((1ull << s) < d) ++s;
+    if (s > 0) {
+      mul = (uint32_t)(((1ull << (31 + s)) + d - 1) / d);
+      shift = s - 1;
+    }
+  }
+  __device__ __forceinline__ uint32_t quotient(uint32_t n) const { return d == 1 ? n : __umulhi(n, mul) >> shift; }
+};
+
 // The rotation of kvp_rope, passed to kernels by value.
 constexpr int kRopePairs = 128;
 struct RopeTable {
@@ -48,6 +64,7 @@ struct RopeArgs {
   int64_t tokens;
   int heads, D;
   int grad;                 // the transpose
+  FastDiv by_units, by_heads;  // of a thread's index (set by launch_rope)
 };
 
 struct AppendRopeArgs {

@@ -14,7 +14,7 @@ __device__ __forceinline__ float load(const float* p) { return *p; }
 __device__ __forceinline__ void store(uint16_t* p, float v) { *p = narrow(v); }
 __device__ __forceinline__ void store(float* p, float v) { *p = v; }
 
-// One thread per pair, or per dim that is not rotated.  A pair is read whole before it is written, so y may be x.
+// Any sizes, strides and alignment: one thread per pair, or per dim that is not rotated.  A pair is read whole before it is written, so y may be x.
 template <class T>
 __global__ __launch_bounds__(256) void rope_pair_kernel(RopeArgs a) {
   const int R = a.table.rotary_dim, units = a.D - R / 2;
@@ -43,9 +43,93 @@ __global__ __launch_bounds__(256) void rope_pair_kernel(RopeArgs a) {
   }
 }
 
+// A head in units of 8 dims, 16 bytes of bf16 a load: in the half layout a unit and the one R / 2 further, in the
+// interleaved one a unit alone; dims that are not rotated follow.  A thread holds one unit of up to N heads of a token,
+// whose sines and cosines (35 instructions a pair) it computes once, while the loads are under way.
+template <class T, bool IL, int N>
+__global__ __launch_bounds__(256) void rope_unit_kernel(RopeArgs a) {
+  const int R = a.table.rotary_dim, turned = IL ? R / 8 : R / 16;
+  const unsigned e = blockIdx.x * 256u + threadIdx.x;
+  const unsigned th = a.by_units.quotient(e), t = a.by_heads.quotient(th);
+  const int u = (int)(e - th * a.by_units.d), h0 = (int)(th - t * a.by_heads.d), step = (int)a.by_heads.d;
+  if (t >= a.tokens) return;
+  const bool pass = u >= turned;
+  const int i0 = pass ? R + (u - turned) * 8 : u * 8, i1 = i0 + R / 2;  // i1: half layout
+  const T* x = reinterpret_cast<const T*>(a.x) + t * a.x_token + h0 * a.x_head;
+  T* y = reinterpret_cast<T*>(a.y) + t * a.y_token + h0 * a.y_head;
+  Eight p[N], q[IL ? 1 : N];
+#pragma unroll
+  for (int n = 0; n < N; ++n)
+    if (h0 + n * step < a.heads) {
+      p[n].load(x + n * step * a.x_head + i0);
+      if (!IL && !pass) q[n].load(x + n * step * a.x_head + i1);
+    }
+  if (!pass) {
+    Turns<IL ? 4 : 8> w;
+    w.set(a.table, IL ? u * 4 : u * 8, a.pos[t]);
+    if (a.grad)
+#pragma unroll
+      for (float& s : w.sn) s = -s;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      if constexpr (IL) turn_neighbours(p[n], w);
+      else turn_halves(p[n], q[n], w);
+    }
+  }
+#pragma unroll
+  for (int n = 0; n < N; ++n)
+    if (h0 + n * step < a.heads) {
+      p[n].store(y + n * step * a.y_head + i0);
+      if (!IL && !pass) q[n].store(y + n * step * a.y_head + i1);
+    }
+}
+
+template <class T>
+bool in_units(const RopeArgs& a) {
+  const int64_t per = 16 / sizeof(T);  // elements of 16 bytes
+  return a.D % 8 == 0 && a.table.rotary_dim % (a.table.interleaved ? 8 : 16) == 0 &&
+         (a.x_token | a.x_head | a.y_token | a.y_head) % per == 0 &&
+         (reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.y)) % 16 == 0;
+}
+
+template <class T, bool IL, int N>
+void launch_units(RopeArgs a, unsigned units, hipStream_t s) {
+  a.by_units = FastDiv(units);
+  a.by_heads = FastDiv((a.heads + N - 1) / N);
+  const int64_t per = (int64_t)a.by_units.d * a.by_heads.d;
+  const int64_t most = std::max<int64_t>(1, (1ll << 30) / per);  // tokens of a launch: 31-bit thread indices
+  for (int64_t t = 0; t < a.tokens; t += most) {
+    RopeArgs b = a;
+    b.tokens = std::min(most, a.tokens - t);
+    b.x = reinterpret_cast<const T*>(a.x) + t * a.x_token;
+    b.y = reinterpret_cast<T*>(a.y) + t * a.y_token;
+    b.pos = a.pos + t;
+    hipLaunchKernelGGL((rope_unit_kernel<T, IL, N>), dim3((unsigned)((b.tokens * per + 255) / 256)), dim3(256), 0, s, b);
+  }
+}
+
+template <class T, bool IL>
+void launch_layout(const RopeArgs& a, hipStream_t s) {
+  const unsigned units = (IL ? a.table.rotary_dim / 8 : a.table.rotary_dim / 16) + (a.D - a.table.rotary_dim) / 8;
+  // Four heads a thread where that still leaves 8 waves a SIMD, one where there is little to do.
+  const int64_t threads = a.tokens * a.heads * units;
+  if (threads >= 4ll << 19 && a.heads >= 4) launch_units<T, IL, 4>(a, units, s);
+  else if (threads >= 2ll << 17 && a.heads >= 2) launch_units<T, IL, 2>(a, units, s);
+  else launch_units<T, IL, 1>(a, units, s);
+}
+
+template <class T>
+bool launch_in_units(const RopeArgs& a, hipStream_t s) {
+  if (!in_units<T>(a)) return false;
+  if (a.table.interleaved) launch_layout<T, true>(a, s);
+  else launch_layout<T, false>(a, s);
+  return true;
+}
+
 }  // namespace
 
 hipError_t launch_rope(const RopeArgs& a, bool f32, hipStream_t s) {
+  if (f32 ? launch_in_units<float>(a, s) : launch_in_units<uint16_t>(a, s)) return hipGetLastError();
   const int64_t n = a.tokens * a.heads * (a.D - a.table.rotary_dim / 2);
   if (n == 0) return hipSuccess;
   const dim3 grid((unsigned)std::min<int64_t>((n + 255) / 256, 1 << 20));

@@ -40,7 +40,70 @@ __device__ __forceinline__ void turn(float p, float q, float sn, float cs, float
   *y1 = fmaf(p, sn, q * cs);
 }
 
+// sin and cos of N consecutive pairs.
+template <int N>
+struct Turns {
+  float sn[N], cs[N];
+  __device__ __forceinline__ void set(const RopeTable& t, int first, int pos) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) pair_turn(t, first + i, pos, &sn[i], &cs[i]);
+  }
+};
+
 __device__ __forceinline__ float widen(uint16_t b) { return __uint_as_float((unsigned)b << 16); }
 __device__ __forceinline__ uint16_t narrow(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }  // to nearest even
+
+
+// 8 consecutive elements of a head, as bf16 or fp32.
+struct Eight {
+  float x[8];
+  __device__ __forceinline__ void load(const uint16_t* p) {
+    typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+    const u32x4 v = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      x[2 * j] = __uint_as_float(v[j] << 16);
+      x[2 * j + 1] = __uint_as_float(v[j] & 0xffff0000u);
+    }
+  }
+  __device__ __forceinline__ void load(const float* p) {
+    const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+    x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+  }
+  __device__ __forceinline__ uint4 bf16() const {
+    typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+    bf16x8 v;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = (__bf16)x[j];
+    return __builtin_bit_cast(uint4, v);
+  }
+  __device__ __forceinline__ void store(uint16_t* p) const { *reinterpret_cast<uint4*>(p) = bf16(); }
+  __device__ __forceinline__ void store(float* p) const {
+    reinterpret_cast<float4*>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
+    reinterpret_cast<float4*>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
+  }
+};
+
+// Pairs (a[j], b[j]): two runs of 8 dims of the half layout.
+__device__ __forceinline__ void turn_halves(Eight& a, Eight& b, const Turns<8>& t) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    float y0, y1;
+    turn(a.x[j], b.x[j], t.sn[j], t.cs[j], &y0, &y1);
+    a.x[j] = y0;
+    b.x[j] = y1;
+  }
+}
+
+// Pairs (a[2 j], a[2 j + 1]): 8 dims of the interleaved layout.
+__device__ __forceinline__ void turn_neighbours(Eight& a, const Turns<4>& t) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    float y0, y1;
+    turn(a.x[2 * j], a.x[2 * j + 1], t.sn[j], t.cs[j], &y0, &y1);
+    a.x[2 * j] = y0;
+    a.x[2 * j + 1] = y1;
+  }
+}
 
 }  // namespace kvp
