@@ -4,6 +4,8 @@
 // of the paper); kv_gather reads tokens back in logical order.  Both work on (page run, kv head) units:
 // one wave moves every token of one sequence that lands in one page, for one KV head, so each unit's
 // writes are whole 16-byte chunks of a single 8 KB page block.
+#include <algorithm>
+
 #include "kvp_kernels.h"
 #include "kvp_layout.h"
 #include "rope_dev.h"
@@ -17,6 +19,32 @@ namespace {
 __device__ __forceinline__ void store_stream(uint16_t* p, uint4 v) {
   typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
   __builtin_nontemporal_store(u32x4{v.x, v.y, v.z, v.w}, reinterpret_cast<u32x4*>(p));
+}
+
+// A wave writes the V block's slots of run r from its tokens' rows in vs [slot][dim]: 2*D chunks, chunk (dt, h, c) holds
+// slots 8h..8h+7 of dim 16*dt + c.
+template <int D>
+__device__ __forceinline__ void put_v(const PageRun& r, const uint16_t* vs, uint16_t* vblk, int lane) {
+  for (int e = lane; e < 2 * D; e += 64) {
+    const int c = e & 15, h = (e >> 4) & 1, dt = e >> 5;
+    const int dim = dt * 16 + c;
+    uint16_t* dst = vblk + v_index<D>(/*token of slot 8h*/ slot_token(8 * h), dim);
+    bool any = false, all = true;
+    for (int j = 0; j < 8; ++j) {
+      const int t = slot_token(8 * h + j);
+      const bool in = t >= r.s_lo && t < r.s_hi;
+      any |= in;
+      all &= in;
+    }
+    if (!any) continue;
+    union { uint4 u; uint16_t s[8]; } val;
+    if (!all) val.u = *reinterpret_cast<const uint4*>(dst);
+    for (int j = 0; j < 8; ++j) {
+      const int t = slot_token(8 * h + j);
+      if (t >= r.s_lo && t < r.s_hi) val.s[j] = vs[t * D + dim];
+    }
+    store_stream(dst, val.u);
+  }
 }
 
 template <int D>
@@ -48,27 +76,7 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a) {
   }
   __builtin_amdgcn_wave_barrier();
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-  // V block: 2*D chunks, chunk (dt, h, c) holds slots 8h..8h+7 of dim 16*dt + c.
-  for (int e = lane; e < 2 * D; e += 64) {
-    const int c = e & 15, h = (e >> 4) & 1, dt = e >> 5;
-    const int dim = dt * 16 + c;
-    uint16_t* dst = vblk + v_index<D>(/*token of slot 8h*/ slot_token(8 * h), dim);
-    bool any = false, all = true;
-    for (int j = 0; j < 8; ++j) {
-      const int t = slot_token(8 * h + j);
-      const bool in = t >= r.s_lo && t < r.s_hi;
-      any |= in;
-      all &= in;
-    }
-    if (!any) continue;
-    union { uint4 u; uint16_t s[8]; } val;
-    if (!all) val.u = *reinterpret_cast<const uint4*>(dst);
-    for (int j = 0; j < 8; ++j) {
-      const int t = slot_token(8 * h + j);
-      if (t >= r.s_lo && t < r.s_hi) val.s[j] = vs[t * D + dim];
-    }
-    store_stream(dst, val.u);
-  }
+  put_v<D>(r, vs, vblk, lane);
 }
 
 // ---------------------------------------------------------------------------------------------------
@@ -97,6 +105,32 @@ __device__ __forceinline__ uint2 quant8(uint4 x, float inv) {
 #pragma unroll
   for (int j = 0; j < 8; ++j) w[j >> 2] |= e4m3_code(bf16_to_f32(h[j]) * inv) << (8 * (j & 3));
   return make_uint2(w[0], w[1]);
+}
+
+// As put_v, quantised.  D pieces of 16 bytes; piece (Y, h, cc) holds slots 8h..8h+7 of dims 32Y + cc and 32Y + 16 + cc.
+template <int D>
+__device__ __forceinline__ void put_v_fp8(const PageRun& r, const uint16_t* vs, uint8_t* vblk, float inv_scale, int lane) {
+  for (int e = lane; e < D; e += 64) {
+    const int cc = e & 15, h = (e >> 4) & 1, Y = e >> 5;
+    uint8_t* dst = vblk + ((Y * 2 + h) * 16 + cc) * 16;
+    bool any = false, all = true;
+    for (int j = 0; j < 8; ++j) {
+      const int t = slot_token(8 * h + j);
+      const bool in = t >= r.s_lo && t < r.s_hi;
+      any |= in;
+      all &= in;
+    }
+    if (!any) continue;
+    union { uint4 u; uint8_t b[16]; } val;
+    if (!all) val.u = *reinterpret_cast<const uint4*>(dst);
+    for (int dh = 0; dh < 2; ++dh)
+      for (int j = 0; j < 8; ++j) {
+        const int t = slot_token(8 * h + j);
+        if (t >= r.s_lo && t < r.s_hi)
+          val.b[dh * 8 + j] = (uint8_t)e4m3_code(bf16_to_f32(vs[t * D + 32 * Y + 16 * dh + cc]) * inv_scale);
+      }
+    store_stream(reinterpret_cast<uint16_t*>(dst), val.u);
+  }
 }
 
 template <int D>
@@ -134,28 +168,7 @@ __global__ __launch_bounds__(256) void append_fp8_kernel(AppendArgs a) {
   }
   __builtin_amdgcn_wave_barrier();
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-  // V: D pieces of 16 bytes; piece (Y, h, cc) holds slots 8h..8h+7 of dims 32Y + cc and 32Y + 16 + cc.
-  for (int e = lane; e < D; e += 64) {
-    const int cc = e & 15, h = (e >> 4) & 1, Y = e >> 5;
-    uint8_t* dst = vblk + ((Y * 2 + h) * 16 + cc) * 16;
-    bool any = false, all = true;
-    for (int j = 0; j < 8; ++j) {
-      const int t = slot_token(8 * h + j);
-      const bool in = t >= r.s_lo && t < r.s_hi;
-      any |= in;
-      all &= in;
-    }
-    if (!any) continue;
-    union { uint4 u; uint8_t b[16]; } val;
-    if (!all) val.u = *reinterpret_cast<const uint4*>(dst);
-    for (int dh = 0; dh < 2; ++dh)
-      for (int j = 0; j < 8; ++j) {
-        const int t = slot_token(8 * h + j);
-        if (t >= r.s_lo && t < r.s_hi)
-          val.b[dh * 8 + j] = (uint8_t)e4m3_code(bf16_to_f32(vs[t * D + 32 * Y + 16 * dh + cc]) * a.inv_scale_v);
-      }
-    store_stream(reinterpret_cast<uint16_t*>(dst), val.u);
-  }
+  put_v_fp8<D>(r, vs, vblk, a.inv_scale_v, lane);
 }
 
 // bf16(fp32(code value) * scale) of the two codes in half `hi` of w.
@@ -240,15 +253,118 @@ __global__ __launch_bounds__(256) void gather_kernel(GatherArgs a) {
   }
 }
 
-// kv_append_rope: one wave per (page run, head), the KV heads first, then the query heads of the same tokens.  A lane
-// turns pairs of one head's dims; a dim that is not rotated is a unit of its own.
-template <int D, bool F8>
+// kv_append_rope.  One wave per (page run, KV head) turns the keys and writes both blocks; one per (page run, up to
+// kQueryHeads query heads) turns the queries of the same tokens.  A lane holds a unit of 8 dims of one token (in the half
+// layout with the unit R / 2 further), computes its sines and cosines once and uses them for all of the wave's heads; a
+// run of few tokens spreads the heads over the lanes.  Bandwidth is what bounds it.
+constexpr int kQueryHeads = 8;
+
+template <int D, bool F8, bool IL>
 __global__ __launch_bounds__(256) void append_rope_kernel(AppendRopeArgs r) {
+  __shared__ uint16_t vstage[4][16 * D];
+  const AppendArgs& a = r.kv;
+  const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const unsigned unit = blockIdx.x * 4u + w, run = r.by_slots.quotient(unit);
+  const int slot = (int)(unit - run * r.by_slots.d);
+  if (run >= (unsigned)a.n_runs) return;
+  const PageRun pr = a.runs[run];
+  const int ntok = pr.s_hi - pr.s_lo;
+  const int R = r.table.rotary_dim, turned = IL ? R / 8 : R / 16, units = turned + (D - R) / 8;
+  const int width = ntok * units > 32 ? 64 : ntok * units > 16 ? 32 : ntok * units > 8 ? 16 : 8;
+
+  if (slot >= a.Hkv) {
+    const int h_lo = (slot - a.Hkv) * kQueryHeads, h_hi = min(h_lo + kQueryHeads, r.Hq);
+    const int across = 64 / width;  // heads at a time
+    for (int e = lane & (width - 1); e < ntok * units; e += width) {
+      const int tt = e / units, u = e - tt * units;
+      const int64_t tok = pr.src0 + tt;
+      const bool pass = u >= turned;
+      const int i0 = pass ? R + (u - turned) * 8 : u * 8;
+      const uint16_t* x = r.q + tok * r.q_stride + i0;
+      uint16_t* y = r.q_out + tok * r.q_out_stride + i0;
+      Turns<IL ? 4 : 8> t;
+      if (!pass) t.set(r.table, IL ? u * 4 : u * 8, pr.lpage * 16 + pr.s_lo + tt);
+      constexpr int N = 4;  // heads whose loads are under way together
+      for (int h = h_lo + lane / width; h < h_hi; h += N * across) {
+        Eight p[N], q[N];
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+          if (h + n * across < h_hi) {
+            p[n].load(x + (h + n * across) * D);
+            if (!IL && !pass) q[n].load(x + (h + n * across) * D + R / 2);
+          }
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+          if (h + n * across < h_hi) {
+            if (!pass) {
+              if constexpr (IL) turn_neighbours(p[n], t);
+              else turn_halves(p[n], q[n], t);
+            }
+            p[n].store(y + (h + n * across) * D);
+            if (!IL && !pass) q[n].store(y + (h + n * across) * D + R / 2);
+          }
+      }
+    }
+    return;
+  }
+
+  const int id = a.bt[(int64_t)pr.row * a.maxp + pr.lpage];
+  if ((unsigned)id >= (unsigned)a.num_pages) {
+    if (lane == 0) atomicCAS(a.err, 0, KVP_ERANGE);
+    return;
+  }
+  const int64_t block = ((int64_t)id * a.Hkv + slot) * (2 * 16 * D);
+  uint8_t* const b8 = reinterpret_cast<uint8_t*>(a.layer) + block;
+  uint16_t* const b16 = a.layer + block;
+  auto put_k = [&](int s, int c, const Eight& v) {  // 8 dims of a token: 16 bytes, or 8 codes
+    if (F8) {
+      unsigned code[2] = {0u, 0u};
+#pragma unroll
+      for (int j = 0; j < 8; ++j) code[j >> 2] |= e4m3_code(v.x[j] * a.inv_scale_k) << (8 * (j & 3));
+      *reinterpret_cast<uint2*>(b8 + k8_index<D>(s, c)) = make_uint2(code[0], code[1]);
+    } else {
+      store_stream(b16 + k_index<D>(s, c), v.bf16());
+    }
+  };
+  uint16_t* vs = vstage[w];
+  constexpr int CH = D / 8;
+  for (int e = lane; e < ntok * CH; e += 64) {
+    const int tt = e / CH, c8 = e - tt * CH;
+    *reinterpret_cast<uint4*>(vs + (pr.s_lo + tt) * D + c8 * 8) =
+        *reinterpret_cast<const uint4*>(a.v + (pr.src0 + tt) * r.v_stride + slot * D + c8 * 8);
+  }
+  for (int e = lane; e < ntok * units; e += 64) {
+    const int tt = e / units, u = e - tt * units, s = pr.s_lo + tt;
+    const uint16_t* x = a.k + (pr.src0 + tt) * r.k_stride + slot * D;
+    const bool pass = u >= turned;
+    const int i0 = pass ? R + (u - turned) * 8 : u * 8;
+    Eight p, q;
+    p.load(x + i0);
+    if (!IL && !pass) q.load(x + i0 + R / 2);
+    if (!pass) {
+      Turns<IL ? 4 : 8> t;
+      t.set(r.table, IL ? u * 4 : u * 8, pr.lpage * 16 + s);
+      if constexpr (IL) turn_neighbours(p, t);
+      else turn_halves(p, q, t);
+    }
+    put_k(s, i0, p);
+    if (!IL && !pass) put_k(s, i0 + R / 2, q);
+  }
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  if (F8) put_v_fp8<D>(pr, vs, b8 + 16 * D, a.inv_scale_v, lane);
+  else put_v<D>(pr, vs, b16 + 16 * D, lane);
+}
+
+// kv_append_rope of a rotary_dim that is not made of whole units: one wave per (page run, head), the KV heads first, then
+// the query heads of the same tokens.  A lane turns pairs of one head's dims; a dim that is not rotated is a unit too.
+template <int D, bool F8>
+__global__ __launch_bounds__(256) void append_rope_pair_kernel(AppendRopeArgs r) {
   const AppendArgs& a = r.kv;
   const int lane = threadIdx.x & 63;
-  const int64_t unit = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int heads = a.Hkv + r.Hq, run = (int)(unit / heads), h = (int)(unit - (int64_t)run * heads);
-  if (run >= a.n_runs) return;
+  const unsigned unit = blockIdx.x * 4u + (threadIdx.x >> 6), run = r.by_slots.quotient(unit);
+  const int h = (int)(unit - run * r.by_slots.d);
+  if (run >= (unsigned)a.n_runs) return;
   const PageRun pr = a.runs[run];
   const int ntok = pr.s_hi - pr.s_lo;
   const bool key = h < a.Hkv;
@@ -332,18 +448,27 @@ hipError_t launch_append(const AppendArgs& a, int D, hipStream_t s) {
   return hipGetLastError();
 }
 
-hipError_t launch_append_rope(const AppendRopeArgs& a, int D, hipStream_t s) {
-  const int64_t units = (int64_t)a.kv.n_runs * (a.kv.Hkv + a.Hq);
-  if (units == 0) return hipSuccess;
-  const dim3 grid((unsigned)((units + 3) / 4));
-  if (a.kv.fp8) {
-    if (D == 128) hipLaunchKernelGGL((append_rope_kernel<128, true>), grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((append_rope_kernel<64, true>), grid, dim3(256), 0, s, a);
-  } else if (D == 128) {
-    hipLaunchKernelGGL((append_rope_kernel<128, false>), grid, dim3(256), 0, s, a);
-  } else {
-    hipLaunchKernelGGL((append_rope_kernel<64, false>), grid, dim3(256), 0, s, a);
+template <int D, bool F8>
+static void launch_append_rope(const AppendRopeArgs& a, hipStream_t s) {
+  const bool whole = a.table.rotary_dim % (a.table.interleaved ? 8 : 16) == 0;
+  const int slots = a.kv.Hkv + (whole ? (a.Hq + kQueryHeads - 1) / kQueryHeads : a.Hq);
+  const int most = (int)((1u << 30) / slots);  // runs of a launch: 31-bit unit indices
+  AppendRopeArgs b = a;
+  b.by_slots = FastDiv(slots);
+  for (int r = 0; r < a.kv.n_runs; r += most) {
+    b.kv.runs = a.kv.runs + r;
+    b.kv.n_runs = std::min(most, a.kv.n_runs - r);
+    const dim3 grid((unsigned)(((int64_t)b.kv.n_runs * slots + 3) / 4));
+    if (!whole) hipLaunchKernelGGL((append_rope_pair_kernel<D, F8>), grid, dim3(256), 0, s, b);
+    else if (a.table.interleaved) hipLaunchKernelGGL((append_rope_kernel<D, F8, true>), grid, dim3(256), 0, s, b);
+    else hipLaunchKernelGGL((append_rope_kernel<D, F8, false>), grid, dim3(256), 0, s, b);
   }
+}
+
+hipError_t launch_append_rope(const AppendRopeArgs& a, int D, hipStream_t s) {
+  if (a.kv.n_runs == 0) return hipSuccess;
+  if (D == 128) a.kv.fp8 ? launch_append_rope<128, true>(a, s) : launch_append_rope<128, false>(a, s);
+  else a.kv.fp8 ? launch_append_rope<64, true>(a, s) : launch_append_rope<64, false>(a, s);
   return hipGetLastError();
 }
 

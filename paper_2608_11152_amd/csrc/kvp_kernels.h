@@ -75,6 +75,7 @@ struct AppendRopeArgs {
   uint16_t* q_out;
   int64_t q_stride, q_out_stride;
   int Hq;
+  FastDiv by_slots;         // of a wave's index (set by launch_append_rope)
 };
 
 // Linear attention over states [slots, Hkv, D, D].  One item is a run of tokens of one sequence.
