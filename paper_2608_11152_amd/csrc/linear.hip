@@ -11,11 +11,13 @@
 // writes o, once.  Bandwidth is what bounds it: 8 D bytes and 6 D^2 .. 10 D^2 flops a token and head.
 //
 // All products run as v_mfma_f32_16x16x32_bf16.  Its result tile gives a lane 4 rows (4 g + r) of one column; its
-// operand wants 8 consecutive k of one row or column.  Two stacked result tiles are such an operand if k is read in the
-// order  slot(8 g + b) = 4 g + b, slot(8 g + 4 + b) = 16 + 4 g + b  (b < 4): the sum over k does not mind.  So the
-// dims of Q and K and the tokens of K^T and V^T lie in that order in LDS, and the state and the weights of a chunk go
-// from one product's result into the next one's operand without leaving their registers:
+// operand wants 8 consecutive k (8 g ..) of one row or column.  Which dim or token a row of a tile stands for is free: row
+// m of an even tile is 8 (m / 4) + m % 4 of its 32, of the odd tile 4 more, so a lane's rows of both are 8 consecutive
+// ones, and the state and the weights of a chunk go from one product's result into the next one's operand without leaving
+// their registers:
 //   P^T (keys x rows)   = K Q^T           O^T (columns x rows) = S^T Q^T + V^T P^T           S (dims x columns) = K^T V
+// Rows of q, k and v go from memory straight to LDS; K^T and V^T come from there through its transposing reads.
+//
 // A sequence that would leave compute units without work is cut into parts (plan_linear): linear_chunk_kernel without its
 // outputs sums each part from zeros, linear_scan_kernel turns the sums into the states before the parts, and the parts are
 // items.  The parts' keys and values are read twice.
@@ -64,9 +66,6 @@ __device__ __forceinline__ int again(int x) {
   return x;
 }
 
-// Position of element x of a 32 block in the order of the operands above.
-__device__ __forceinline__ int slot_of(int x) { return ((x >> 2) & 3) * 8 + ((x >> 4) & 1) * 4 + (x & 3); }
-
 __device__ double power(double x, unsigned n) {
   double y = 1.0;
   for (; n; n >>= 1, x *= x)
@@ -76,55 +75,72 @@ __device__ double power(double x, unsigned n) {
 
 constexpr int kChunk = 64;  // tokens
 
+// A tile in LDS: 64 rows (tokens) of D elements.  The 16-byte pieces of a row are keyed by an exclusive or with the row,
+// so that the reads of a tile hit all banks: one piece of 16 rows (16 in a row, or m / 4 of 8 apart), where the hardware
+// serves lanes of two neighbouring pieces together; or halves of 4 pieces of 8 rows (two rows share their banks then).
+template <int D>
+__device__ __forceinline__ int tile_key(int row) {
+  const int b = row ^ (row >> 2);  // bit 2: bits 2 and 4 of the row
+  return D == 128 ? (row & 1) + 2 * ((b >> 2) & 1) + 4 * ((row >> 1) & 1) + (row & 8)
+                  : ((row >> 1) & 1) + 2 * ((b >> 2) & 1) + 4 * ((row >> 3) & 1);
+}
+template <int D>
+__device__ __forceinline__ int tile_at(int row, int piece) {  // in bytes
+  return 2 * D * row + 16 * (piece ^ tile_key<D>(row));
+}
+// tile_at of a row 4 y + 16 x + 32 z further (y and x 0 or 1, the row's bits 2 and 4 clear), from the row's own
+template <int D>
+__device__ __forceinline__ int later(int at, int y, int x, int z) {
+  return (at ^ (32 * (x ^ y))) + 2 * D * (4 * y + 16 * x + 32 * z);
+}
+
+constexpr int kPwsBase = 31;
 template <int D>
 struct Tiles {
-  uint16_t q[kChunk][D + 8];   // rows of tokens, dims in slot order.  The 16 bytes behind each row spread the 16 rows
-  uint16_t k[kChunk][D + 8];   // that a wave reads at a time over all banks
-  uint16_t kt[D][kChunk + 8];  // rows of dims, tokens in slot order
-  uint16_t vt[D][kChunk + 8];
-  float pw[kChunk + 1];        // decay^n
+  unsigned char q[2 * D * kChunk], k[2][2 * D * kChunk], v[2 * D * kChunk];
+  float pw[2 * kChunk];             // decay^(e - 63), 0 below
+  float pws[kChunk + 1 + kPwsBase];  // scale decay^(e - kPwsBase), 0 below
 };
 
-// Where piece p (8 tokens) of a row of K^T or V^T lies in its row.  Rows are 36 words apart: a wave writes one piece of
-// rows 8 apart (32 words: two bank groups without this), and reads rows m, or 8 (m / 4) + m % 4, of one tile.
-__device__ __forceinline__ int piece_at(int row, int p) { return 8 * (p ^ ((row >> 2) & 4) ^ ((row >> 5) & 3)); }
-
-// 8 rows (tokens) of 8 elements become 8 rows (dims) of 8 tokens, and go to LDS.
-template <int P>
-__device__ __forceinline__ void store_transposed(uint16_t (*dst)[P], int dim, int piece, const u32x4* row) {
-  const int at = piece_at(dim, piece);  // dim is a multiple of 8: the same for all 8 rows
-#pragma unroll
-  for (int d = 0; d < 8; ++d) {
-    u32x4 w;
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      w[j] = __builtin_amdgcn_perm(row[2 * j + 1][d >> 1], row[2 * j][d >> 1], d & 1 ? 0x07060302u : 0x05040100u);
-    *reinterpret_cast<u32x4*>(&dst[dim + d][at]) = w;
-  }
+__device__ __forceinline__ u32x4 ld16(const unsigned char* p) { return *reinterpret_cast<const u32x4*>(p); }
+// The LDS's transposing read: of every 16 lanes, lanes 4 r .. 4 r + 3 name 4 elements each of a row r, and lane l gets
+// element l of the 4 rows.  Here the rows are tokens 32 z + 8 g .. + 3 and .. + 7 of the even and of the odd tile of a pair
+// (8 bytes further), so a lane gets operands of 8 tokens.  In assembly, with its wait: before the builtin the compiler
+// waits for all loads to LDS that are under way, whichever tile they go to.
+__device__ __forceinline__ unsigned lds_at(const unsigned char* p) {
+  return (unsigned)(uintptr_t)(__attribute__((address_space(3))) const unsigned char*)p;
+}
+template <int D, int Z>
+__device__ __forceinline__ void ld_columns(unsigned tile, int at, u32x4 out[2]) {
+  u32x2 a, b, c, d;
+  asm volatile(
+      "ds_read_b64_tr_b16 %0, %4 offset:%6\n\t"
+      "ds_read_b64_tr_b16 %1, %5 offset:%7\n\t"
+      "ds_read_b64_tr_b16 %2, %4 offset:%8\n\t"
+      "ds_read_b64_tr_b16 %3, %5 offset:%9\n\t"
+      "s_waitcnt lgkmcnt(0)"
+      : "=&v"(a), "=&v"(b), "=&v"(c), "=&v"(d)
+      : "v"(tile + at), "v"(tile + (at ^ 32)), "n"(64 * D * Z), "n"(64 * D * Z + 8 * D), "n"(64 * D * Z + 8),
+        "n"(64 * D * Z + 8 * D + 8)
+      : "memory");
+  out[0] = u32x4{a[0], a[1], b[0], b[1]};
+  out[1] = u32x4{c[0], c[1], d[0], d[1]};
 }
 
-// 8 dims of one token, in slot order: two pieces of 4.
-template <int P>
-__device__ __forceinline__ void store_row(uint16_t (*dst)[P], int token, int dim, u32x4 v) {
-  uint16_t* p = &dst[token][(dim & ~31) + slot_of(dim & 31)];
-  *reinterpret_cast<u32x2*>(p) = u32x2{v[0], v[1]};
-  *reinterpret_cast<u32x2*>(p + 8) = u32x2{v[2], v[3]};
+// A wave's share of a tile from memory straight to LDS, 1 KB at a time: with W waves, rows 1024 / (2 D) (w + W j) ..,
+// 16 bytes a lane.  The last rows of an item may end inside the tile: rows from n on repeat row n - 1 and are cleared later.
+template <int D>
+__device__ __forceinline__ void fetch_tile(unsigned char* tile, const uint16_t* head, int stride, int n, int w, int lane) {
+  constexpr int PL = D / 8, RW = 64 / PL;  // lanes of a row, rows of a wave
+  const int row = again(RW * w + lane / PL), src = 16 * ((lane % PL) ^ tile_key<D>(row));
+  const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(
+      const_cast<uint16_t*>(head), 0, 2 * ((kChunk - 1) * stride + D), 0x00020000);
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(
+        rsrc, (__attribute__((address_space(3))) void*)(tile + 1024 * w + 32 * D * j), 16,
+        2 * stride * min(row + 16 * j, n - 1) + (src ^ (32 * (j & 1))), 0, 0, 0);
 }
-
-__device__ __forceinline__ u32x4 ld16(const uint16_t* p) { return *reinterpret_cast<const u32x4*>(p); }
-
-// Up to a chunk's rows of one head, as a buffer: reads behind the last row give zeros, writes there are dropped.
-struct Rows {
-  __amdgpu_buffer_rsrc_t rsrc;
-  __device__ __forceinline__ Rows(const void* p, int64_t stride, int rows, int D, int bytes = 2)
-      : rsrc(__builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0,
-                                               rows > 0 ? ((min(rows, kChunk) - 1) * (int)stride + D) * bytes : 0,
-                                               0x00020000)) {}
-  __device__ __forceinline__ u32x4 load(int at) const { return __builtin_amdgcn_raw_buffer_load_b128(rsrc, at, 0, 0); }
-  __device__ __forceinline__ void store(int at, u32x4 v) const {
-    __builtin_amdgcn_raw_buffer_store_b128(v, rsrc, at, 0, 0);
-  }
-};
 
 // State of an item: a slot of the caller's, a part of the workspace (-2, -3, ..), or none (-1).
 __device__ __forceinline__ float* state_at(const LinearArgs& a, int slot, int h, int D) {
@@ -141,44 +157,25 @@ __global__ __launch_bounds__(2 * D, 2) void linear_chunk_kernel(LinearArgs a, Li
   const int item = blockIdx.x / a.Hkv, h = blockIdx.x - item * a.Hkv, G = kAttend ? a.Hq / a.Hkv : 1;
   const LinearItem it = list.items[item];
   const double l1 = (double)list.decay[h];
-  if (tid <= kChunk) L.pw[tid] = (float)power(l1, tid);
+  if (tid <= kChunk) {
+    const double x = power(l1, tid);
+    L.pw[tid + 63] = (float)x;
+    L.pws[tid + kPwsBase] = (float)(a.scale * x);
+  }
+  if (tid < 63) L.pw[tid] = 0.0f;
+  if (tid < kPwsBase) L.pws[tid] = 0.0f;
 
-  // Column n of the wave's 16-wide tile nt is column 8 (n / 4) + 4 nt + n % 4 of its 32: a lane's rows of O^T from
-  // both tiles are then 8 consecutive columns.
   const int col = 32 * w + 8 * (m >> 2) + (m & 3);
   f32x4 S[MT][2] = {};
   if (it.src != -1) {
-    const float* from = state_at(a, it.src, h, D) + 4 * g * D + col;
+    const float* from = state_at(a, it.src, h, D) + 8 * g * D + col;
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
       for (int nt = 0; nt < 2; ++nt)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) S[mt][nt][r] = from[(16 * mt + r) * D + 4 * nt];
+        for (int r = 0; r < 4; ++r) S[mt][nt][r] = from[(32 * (mt >> 1) + 4 * (mt & 1) + r) * D + 4 * nt];
   }
-
-  // What a thread brings: an 8 x 8 block of k (the first D threads) or v, and 4 pieces of q.  Rows behind the item's
-  // last are outside their buffer and read as zeros.
-  const int c8 = (tid % (D / 8)) * 8, tg = (tid % D) / (D / 8), first = 32 * (tg >> 2) + 4 * (tg & 3);
-  const bool keys = w < D / 64;
-  const uint16_t* const kv = keys ? a.k : a.v;
-  const int64_t kv_stride = keys ? a.k_stride : a.v_stride;
-  const int qrow = tid / (D / 8);
-  u32x4 rkv[8], rq[4];
-  auto fetch_kv = [&](int c) {
-    const Rows rows(kv + (it.t0 + (int64_t)c) * kv_stride + h * D, kv_stride, it.n - c, D);
-    const int at = again(2 * (first * (int)kv_stride + c8));
-#pragma unroll
-    for (int j = 0; j < 8; ++j) rkv[j] = rows.load(at + 2 * ((j & 3) + 4 * (j & 4)) * (int)kv_stride);
-  };
-  auto fetch_q = [&](int c, int gq) {
-    const Rows rows(a.q + (it.t0 + (int64_t)c) * a.q_stride + (h * G + gq) * D, a.q_stride, it.n - c, D);
-    const int at = again(2 * (qrow * (int)a.q_stride + c8));
-#pragma unroll
-    for (int j = 0; j < 4; ++j) rq[j] = rows.load(at + 32 * j * (int)a.q_stride);
-  };
-  fetch_kv(0);
-  if (kAttend) fetch_q(0, 0);
 
   // The state's decay over a chunk, l^64 rounded to fp32, would be off the same way at every chunk.  `off` is the
   // product of the factors so far over the true one, within a step of fp32 of 1; each factor takes it back.
@@ -186,32 +183,42 @@ __global__ __launch_bounds__(2 * D, 2) void linear_chunk_kernel(LinearArgs a, Li
   const bool track = l64 > 1e-30;
   double off = 1.0;
 
-  for (int c = 0; c < it.n; c += kChunk) {
+  const int q_read = tile_at<D>(m, g), k_read = tile_at<D>(8 * (m >> 2) + (m & 3), g);
+  const int kt_read = tile_at<D>(8 * g + (m >> 2), m & 3), vt_read = tile_at<D>(8 * g + (m >> 2), 4 * w + (m & 3));
+  auto arrived = [&]() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
+  auto all_read = [&]() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
+  auto fetch = [&](unsigned char* tile, const uint16_t* x, int64_t stride, int head, int c) {
+    if (c < it.n)
+      fetch_tile<D>(tile, x + (it.t0 + (int64_t)c) * stride + head * D, (int)stride, min(kChunk, it.n - c), w, lane);
+  };
+
+  // Loads are under way while there is work that does not need them: v during the products with q, the next q and k (which
+  // has two places) from there to the end of the chunk.
+  if (kAttend) fetch(L.q, a.q, a.q_stride, h * G, 0);
+  fetch(L.k[0], a.k, a.k_stride, h, 0);
+  for (int c = 0, odd = 0; c < it.n; c += kChunk, odd ^= 1) {
     const int n = min(kChunk, it.n - c);
-    __syncthreads();
-    if (keys) {
-      store_transposed(L.kt, c8, tg, rkv);
-      if (kAttend)
+    const unsigned char* const Lk = L.k[odd];
+    u32x4 vf[2][2];  // V^T: [32 tokens][16 columns]
+    for (int gq = 0; gq < G; ++gq) {
+      arrived();  // q and k; and the chunk before is done with v
+      if (gq == 0) fetch(L.v, a.v, a.v_stride, h, c);
+      // O^T = S^T Q^T and P^T = K Q^T for the chunk's four row tiles.  Lane column m is row i = 16 rt + m; the rows of P^T
+      // are keys j = 32 (jt / 2) + 4 (jt % 2) + 8 g + r, and later halves than the row's are left out.
+      f32x4 O[4][2] = {}, P[4][4] = {};
 #pragma unroll
-        for (int j = 0; j < 8; ++j) store_row(L.k, first + (j & 3) + 4 * (j & 4), c8, rkv[j]);
-    } else {
-      store_transposed(L.vt, c8, tg, rkv);
-    }
-    if (kAttend) {
-      for (int gq = 0; gq < G; ++gq) {
-        if (gq > 0) __syncthreads();
-#pragma unroll
-        for (int j = 0; j < 4; ++j) store_row(L.q, qrow + 16 * j, c8, rq[j]);
-        __syncthreads();
-        if (gq + 1 < G) fetch_q(c, gq + 1);
-        // O^T = S^T Q^T for the chunk's four row tiles
-        f32x4 O[4][2] = {};
+      for (int mt = 0; mt < MT; ++mt) asm volatile("" : "+v"(S[mt][0]), "+v"(S[mt][1]));  // (not split once for all heads)
+      if (kAttend) {
+        const int q_at = again(q_read), k_at = again(k_read);
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
           __builtin_amdgcn_sched_barrier(0);
-          u32x4 qf[4];
+          u32x4 qf[4], kf[4];
 #pragma unroll
-          for (int rt = 0; rt < 4; ++rt) qf[rt] = ld16(&L.q[16 * rt + m][32 * ks + 8 * g]);
+          for (int rt = 0; rt < 4; ++rt) {
+            qf[rt] = ld16(L.q + later<D>(q_at ^ (64 * ks), 0, rt & 1, rt >> 1));
+            kf[rt] = ld16(Lk + later<D>(k_at ^ (64 * ks), rt & 1, 0, rt >> 1));
+          }
 #pragma unroll
           for (int nt = 0; nt < 2; ++nt) {
             u32x4 hi, lo;
@@ -226,111 +233,121 @@ __global__ __launch_bounds__(2 * D, 2) void linear_chunk_kernel(LinearArgs a, Li
 #pragma unroll
             for (int rt = 0; rt < 4; ++rt) O[rt][nt] = mfma16(lo, qf[rt], O[rt][nt]);
           }
+#pragma unroll
+          for (int rt = 0; rt < 4; ++rt)
+#pragma unroll
+            for (int jt = 0; jt < 2 * (rt / 2) + 2; ++jt) P[rt][jt] = mfma16(kf[jt], qf[rt], P[rt][jt]);
         }
-        const int es = a.out_f32 ? 4 : 2;
-        const Rows out(reinterpret_cast<char*>(a.out) + ((it.t0 + (int64_t)c) * a.Hq + h * G + gq) * D * es, a.Hq * D,
-                       n, D, es);
-        bool bad = false;
+      }
+      arrived();  // v; and q has been read
+      if (gq == 0 && n < kChunk) {  // the rows that stand in for those behind the last: v must not count
+        for (int e = tid; e < (kChunk - n) * (D / 8); e += 2 * D)
+          *reinterpret_cast<u32x4*>(L.v + 2 * D * n + 16 * e) = u32x4{0, 0, 0, 0};
+        all_read();
+      }
+      if (gq == G - 1) {
+        if (kAttend) fetch(L.q, a.q, a.q_stride, h * G, c + kChunk);
+        fetch(L.k[odd ^ 1], a.k, a.k_stride, h, c + kChunk);
+      } else {
+        fetch(L.q, a.q, a.q_stride, h * G + gq + 1, c);
+      }
+      if (!kAttend) break;
+      const int es = a.out_f32 ? 4 : 2;
+      char* const out = reinterpret_cast<char*>(a.out) + ((it.t0 + (int64_t)c) * a.Hq + h * G + gq) * D * es;
+      bool bad = false;
+      ld_columns<D, 0>(lds_at(L.v), vt_read, vf[0]);
+      ld_columns<D, 1>(lds_at(L.v), vt_read, vf[1]);
 #pragma unroll
-        for (int rt = 3; rt >= 0; --rt) {
-          __builtin_amdgcn_sched_barrier(0);
-          // P^T: lane column m is row i = 16 rt + m, its rows are keys j = 16 jt + 4 g + r
-          const int g8 = again(8 * g), m4 = again(m - 4 * g);
-          f32x4 P[4] = {};
+      for (int rt = 3; rt >= 0; --rt) {
+        __builtin_amdgcn_sched_barrier(0);
+        const int mg = again(m - 8 * g);
 #pragma unroll
-          for (int ks = 0; ks < KS; ++ks) {
-            const u32x4 qf = ld16(&L.q[16 * rt + m][32 * ks + g8]);
+        for (int jt = 0; jt < 2 * (rt / 2) + 2; ++jt)
 #pragma unroll
-            for (int jt = 0; jt <= rt; ++jt) P[jt] = mfma16(ld16(&L.k[16 * jt + m][32 * ks + g8]), qf, P[jt]);
+          for (int r = 0; r < 4; ++r) {
+            const bool whole = jt / 2 < rt / 2;  // all of these keys are before all of the rows
+            const int e = mg + 16 * rt - 32 * (jt >> 1) - 4 * (jt & 1) - r;
+            P[rt][jt][r] *= L.pws[e + kPwsBase];
+            if (!whole && e < 0) P[rt][jt][r] = 0.0f;
+          }
+        f32x4 V[2] = {};
+#pragma unroll
+        for (int s = 0; s <= rt / 2; ++s) {
+          u32x4 hi, lo;
+#pragma unroll
+          for (int b = 0; b < 4; ++b) {
+            float x = P[rt][2 * s + (b >> 1)][2 * (b & 1)], y = P[rt][2 * s + (b >> 1)][2 * (b & 1) + 1];
+            hi[b] = part(x, y);
+            lo[b] = pack2(x, y);
           }
 #pragma unroll
-          for (int jt = 0; jt <= rt; ++jt)
+          for (int nt = 0; nt < 2; ++nt) V[nt] = mfma16(vf[s][nt], hi, V[nt]);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              const int e = m4 + 16 * (rt - jt) - r;
-              P[jt][r] *= a.scale * L.pw[jt < rt ? e : max(e, 0)];
-              if (jt == rt && e < 0) P[jt][r] = 0.0f;
-            }
-          f32x4 V[2] = {};
+          for (int nt = 0; nt < 2; ++nt) V[nt] = mfma16(vf[s][nt], lo, V[nt]);
+        }
+        if (rt == 3) {
+          // A value of v that is not finite gives no number in the chunk's last row, and, as 0 times it, in earlier
+          // rows that must not see it.
+          float z = 0.0f;
 #pragma unroll
-          for (int s = 0; s <= rt / 2; ++s) {
-            u32x4 hi, lo;
-#pragma unroll
-            for (int b = 0; b < 4; ++b) {
-              float x = P[2 * s + (b >> 1)][2 * (b & 1)], y = P[2 * s + (b >> 1)][2 * (b & 1) + 1];
-              hi[b] = part(x, y);
-              lo[b] = pack2(x, y);
-            }
-#pragma unroll
-            for (int nt = 0; nt < 2; ++nt) {
-              const u32x4 vf = ld16(&L.vt[col + 4 * nt][piece_at(col, 4 * s + (g8 >> 3))]);
-              V[nt] = mfma16(vf, hi, V[nt]);
-              V[nt] = mfma16(vf, lo, V[nt]);
-            }
-          }
-          if (rt == 3) {
-            // A value of v that is not finite gives no number in the chunk's last row, and, as 0 times it, in earlier
-            // rows that must not see it.
-            float z = 0.0f;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) z += (V[0][r] - V[0][r]) + (V[1][r] - V[1][r]);
-            if (__any(z != 0.0f)) {
-              float y = 0.0f;
+          for (int r = 0; r < 4; ++r) z += (V[0][r] - V[0][r]) + (V[1][r] - V[1][r]);
+          if (__any(z != 0.0f)) {
+            float y = 0.0f;
 #pragma unroll 1
-              for (int s = 0; s < 4; ++s) {
-                const u32x4 v = ld16(&L.vt[32 * w + (lane >> 1)][32 * (lane & 1) + 8 * s]);  // any order will do
+            for (int s = 0; s < 4; ++s) {
+              const u32x4 v = ld16(L.v + tile_at<D>(lane, 4 * w + s));
 #pragma unroll
-                for (int b = 0; b < 4; ++b) y += (low(v[b]) - low(v[b])) + (high(v[b]) - high(v[b]));
-              }
-              bad = __any(y != 0.0f);
+              for (int b = 0; b < 4; ++b) y += (low(v[b]) - low(v[b])) + (high(v[b]) - high(v[b]));
             }
+            bad = __any(y != 0.0f);
           }
-          const int i = 16 * rt + m;
-          if (bad) {  // key by key: only keys up to the row are multiplied at all
-            V[0] = V[1] = f32x4{};
+        }
+        const int i = 16 * rt + m;
+        if (bad) {  // key by key: only keys up to the row are multiplied at all
+          const uint16_t* const qi = a.q + (it.t0 + (int64_t)(c + min(i, n - 1))) * a.q_stride + (h * G + gq) * D;
+          V[0] = V[1] = f32x4{};
 #pragma unroll 1
-            for (int j = 0; j < 16 * rt + 16; ++j) {
-              float p = 0.0f;
+          for (int j = 0; j < 16 * rt + 16; ++j) {
+            float p = 0.0f;
 #pragma unroll 1
-              for (int d = 0; d < D; d += 8) {
-                const u32x4 x = ld16(&L.q[i][d]), y = ld16(&L.k[j][d]);
+            for (int d = 0; d < D / 8; ++d) {
+              const u32x4 x = *reinterpret_cast<const u32x4*>(qi + 8 * d), y = ld16(Lk + tile_at<D>(j, d));
 #pragma unroll
-                for (int b = 0; b < 4; ++b) p = fmaf(high(x[b]), high(y[b]), fmaf(low(x[b]), low(y[b]), p));
-              }
-              p *= a.scale * L.pw[max(i - j, 0)];
-#pragma unroll
-              for (int x = 0; x < 8; ++x) {
-                const int row = 32 * w + 8 * g + x, at = (j & 32) + slot_of(j & 31);
-                const float v = widen(L.vt[row][piece_at(row, at >> 3) + (at & 7)]);
-                if (j <= i) V[x >> 2][x & 3] = fmaf(p, v, V[x >> 2][x & 3]);
-              }
+              for (int b = 0; b < 4; ++b) p = fmaf(high(x[b]), high(y[b]), fmaf(low(x[b]), low(y[b]), p));
             }
+            p *= L.pws[i - j + kPwsBase > 0 ? i - j + kPwsBase : 0];
+            const u32x4 v = ld16(L.v + tile_at<D>(j, 4 * w + g));
+#pragma unroll
+            for (int x = 0; x < 8; ++x)
+              if (j <= i) V[x >> 2][x & 3] = fmaf(p, x & 1 ? high(v[x >> 1]) : low(v[x >> 1]), V[x >> 2][x & 3]);
           }
-          const float f = a.scale * L.pw[again(i + 1)];
+        }
+        const float f = L.pws[again(i + 1) + kPwsBase];
 #pragma unroll
-          for (int nt = 0; nt < 2; ++nt)
+        for (int nt = 0; nt < 2; ++nt)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) V[nt][r] = fmaf(O[rt][nt][r], f, V[nt][r]);
+          for (int r = 0; r < 4; ++r) V[nt][r] = fmaf(O[rt][nt][r], f, V[nt][r]);
+        if (i < n) {
           const int at = again(i) * a.Hq * D + 32 * w + 8 * g;
           if (a.out_f32) {
-            out.store(4 * at, __builtin_bit_cast(u32x4, V[0]));
-            out.store(4 * at + 16, __builtin_bit_cast(u32x4, V[1]));
+            f32x4* o = reinterpret_cast<f32x4*>(out + 4 * (int64_t)at);
+            o[0] = V[0];
+            o[1] = V[1];
           } else {
-            out.store(2 * at, u32x4{pack2(V[0][0], V[0][1]), pack2(V[0][2], V[0][3]), pack2(V[1][0], V[1][1]),
-                                    pack2(V[1][2], V[1][3])});
+            *reinterpret_cast<u32x4*>(out + 2 * (int64_t)at) =
+                u32x4{pack2(V[0][0], V[0][1]), pack2(V[0][2], V[0][3]), pack2(V[1][0], V[1][1]), pack2(V[1][2], V[1][3])};
           }
         }
       }
-    } else {
-      __syncthreads();
     }
-    // The next chunk's rows, which arrive during the update of the state.
-    fetch_kv(c + kChunk);
-    if (kAttend) fetch_q(c + kChunk, 0);
     __builtin_amdgcn_sched_barrier(0);
-    const int g8 = again(8 * g);
-    // S = l^n S + (l^(n-1-j) V's rows times K^T); rows from n on are zeros
-    float keep = L.pw[n];
+    if (!kAttend) {
+      ld_columns<D, 0>(lds_at(L.v), vt_read, vf[0]);
+      ld_columns<D, 1>(lds_at(L.v), vt_read, vf[1]);
+    }
+    const int last = again(n - 1 - 8 * g);
+    // S = l^n S + K^T (l^(n-1-j) v_j); rows from n on are zeros
+    float keep = L.pw[n + 63];
     if (n == kChunk && track) {
       keep = (float)(l64 * (2.0 - off));
       off *= (double)keep * back;
@@ -344,14 +361,13 @@ __global__ __launch_bounds__(2 * D, 2) void linear_chunk_kernel(LinearArgs a, Li
       __builtin_amdgcn_sched_barrier(0);
       float d[8];
 #pragma unroll
-      for (int b = 0; b < 8; ++b) d[b] = L.pw[max(n - 1 - (32 * s + (g8 >> 1) + (b & 3) + 4 * (b & 4)), 0)];
+      for (int b = 0; b < 8; ++b) d[b] = L.pw[last - (32 * s + b) + 63];
       u32x4 vp[2][3];
 #pragma unroll
       for (int nt = 0; nt < 2; ++nt) {
-        const u32x4 vf = ld16(&L.vt[col + 4 * nt][piece_at(col, 4 * s + (g8 >> 3))]);
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
-          float x = low(vf[b]) * d[2 * b], y = high(vf[b]) * d[2 * b + 1];
+          float x = low(vf[s][nt][b]) * d[2 * b], y = high(vf[s][nt][b]) * d[2 * b + 1];
           vp[nt][0][b] = part(x, y);
           vp[nt][1][b] = part(x, y);
           vp[nt][2][b] = pack2(x, y);
@@ -360,8 +376,9 @@ __global__ __launch_bounds__(2 * D, 2) void linear_chunk_kernel(LinearArgs a, Li
       // Four independent sums at a time: one product's result is the next but three's summand.
 #pragma unroll
       for (int mt = 0; mt < MT; mt += 2) {
-        const u32x4 kf[2] = {ld16(&L.kt[16 * mt + m][piece_at(16 * mt, 4 * s + (g8 >> 3))]),
-                             ld16(&L.kt[16 * mt + 16 + m][piece_at(16 * mt + 16, 4 * s + (g8 >> 3))])};
+        u32x4 kf[2];
+        if (s == 0) ld_columns<D, 0>(lds_at(Lk), kt_read ^ (32 * mt), kf);
+        else ld_columns<D, 1>(lds_at(Lk), kt_read ^ (32 * mt), kf);
 #pragma unroll
         for (int x = 2; x >= 0; --x)
 #pragma unroll
@@ -370,13 +387,13 @@ __global__ __launch_bounds__(2 * D, 2) void linear_chunk_kernel(LinearArgs a, Li
     }
   }
   if (it.dst == -1) return;
-  float* to = state_at(a, it.dst, h, D) + 4 * g * D + col;
+  float* to = state_at(a, it.dst, h, D) + 8 * g * D + col;
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
     for (int nt = 0; nt < 2; ++nt)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) to[(16 * mt + r) * D + 4 * nt] = S[mt][nt][r];
+      for (int r = 0; r < 4; ++r) to[(32 * (mt >> 1) + 4 * (mt & 1) + r) * D + 4 * nt] = S[mt][nt][r];
 }
 
 // States before each part of the long sequences, from the parts' own sums: S_0 = source, S_i = l^len S_(i-1) + sum_(i-1).
