@@ -54,7 +54,8 @@ __device__ __forceinline__ float high(unsigned w) { return __uint_as_float(w & 0
 
 // The bf16 of x and y, packed; x and y become what is left of them.
 __device__ __forceinline__ unsigned part(float& x, float& y) {
-  const unsigned w = pack2(x, y);
+  unsigned w = pack2(x, y);
+  asm("" : "+v"(w));  // (or x is converted a second time, alone)
   x -= low(w);
   y -= high(w);
   return w;
@@ -135,11 +136,18 @@ __device__ __forceinline__ void fetch_tile(unsigned char* tile, const uint16_t* 
   const int row = again(RW * w + lane / PL), src = 16 * ((lane % PL) ^ tile_key<D>(row));
   const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(
       const_cast<uint16_t*>(head), 0, 2 * ((kChunk - 1) * stride + D), 0x00020000);
-#pragma unroll
-  for (int j = 0; j < 4; ++j)
+  auto put = [&](int j, int from, int uniform) {
     __builtin_amdgcn_raw_ptr_buffer_load_lds(
-        rsrc, (__attribute__((address_space(3))) void*)(tile + 1024 * w + 32 * D * j), 16,
-        2 * stride * min(row + 16 * j, n - 1) + (src ^ (32 * (j & 1))), 0, 0, 0);
+        rsrc, (__attribute__((address_space(3))) void*)(tile + 1024 * w + 32 * D * j), 16, from, uniform, 0, 0);
+  };
+  if (n == kChunk) {
+    const int even = 2 * stride * row + src, odd = 2 * stride * row + (src ^ 32);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) put(j, j & 1 ? odd : even, 32 * stride * j);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) put(j, 2 * stride * min(row + 16 * j, n - 1) + (src ^ (32 * (j & 1))), 0);
+  }
 }
 
 // State of an item: a slot of the caller's, a part of the workspace (-2, -3, ..), or none (-1).
@@ -290,7 +298,7 @@ __global__ __launch_bounds__(2 * D, 2) void linear_chunk_kernel(LinearArgs a, Li
           // rows that must not see it.
           float z = 0.0f;
 #pragma unroll
-          for (int r = 0; r < 4; ++r) z += (V[0][r] - V[0][r]) + (V[1][r] - V[1][r]);
+          for (int r = 0; r < 4; ++r) z = fmaf(V[0][r], 0.0f, fmaf(V[1][r], 0.0f, z));
           if (__any(z != 0.0f)) {
             float y = 0.0f;
 #pragma unroll 1
