@@ -96,9 +96,9 @@ __device__ __forceinline__ int later(int at, int y, int x, int z) {
 }
 
 constexpr int kPwsBase = 31;
-template <int D>
+template <int D, bool kAttend>
 struct Tiles {
-  unsigned char q[2 * D * kChunk], k[2][2 * D * kChunk], v[2 * D * kChunk];
+  unsigned char q[kAttend ? 2 * D * kChunk : 16], k[2][2 * D * kChunk], v[2 * D * kChunk];
   float pw[2 * kChunk];             // decay^(e - 63), 0 below
   float pws[kChunk + 1 + kPwsBase];  // scale decay^(e - kPwsBase), 0 below
 };
@@ -158,8 +158,8 @@ __device__ __forceinline__ float* state_at(const LinearArgs& a, int slot, int h,
 
 // kAttend: outputs and state; otherwise only the state, from zeros (the sum of a part of a long sequence).
 template <int D, bool kAttend>
-__global__ __launch_bounds__(2 * D, 2) void linear_chunk_kernel(LinearArgs a, LinearItems list) {
-  __shared__ Tiles<D> L;
+__global__ __launch_bounds__(2 * D, kAttend ? 2 : 3) void linear_chunk_kernel(LinearArgs a, LinearItems list) {
+  __shared__ Tiles<D, kAttend> L;
   constexpr int KS = D / 32, MT = D / 16;  // k-steps and row tiles over the dims of k
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, m = lane & 15, g = lane >> 4;
   const int item = blockIdx.x / a.Hkv, h = blockIdx.x - item * a.Hkv, G = kAttend ? a.Hq / a.Hkv : 1;
@@ -194,23 +194,26 @@ __global__ __launch_bounds__(2 * D, 2) void linear_chunk_kernel(LinearArgs a, Li
   const int q_read = tile_at<D>(m, g), k_read = tile_at<D>(8 * (m >> 2) + (m & 3), g);
   const int kt_read = tile_at<D>(8 * g + (m >> 2), m & 3), vt_read = tile_at<D>(8 * g + (m >> 2), 4 * w + (m & 3));
   auto arrived = [&]() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
+  // All loads but the last four, which are v's: fetch_tile is four.
+  auto arrived_but_v = [&]() { asm volatile("s_waitcnt vmcnt(4) lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
   auto all_read = [&]() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
   auto fetch = [&](unsigned char* tile, const uint16_t* x, int64_t stride, int head, int c) {
     if (c < it.n)
       fetch_tile<D>(tile, x + (it.t0 + (int64_t)c) * stride + head * D, (int)stride, min(kChunk, it.n - c), w, lane);
   };
 
-  // Loads are under way while there is work that does not need them: v during the products with q, the next q and k (which
-  // has two places) from there to the end of the chunk.
+  // Loads are under way while there is work that does not need them: the next q and k (which has two places) from the end
+  // of the products with q on, the next v from when the outputs are written until the next products with q are done.
   if (kAttend) fetch(L.q, a.q, a.q_stride, h * G, 0);
   fetch(L.k[0], a.k, a.k_stride, h, 0);
+  fetch(L.v, a.v, a.v_stride, h, 0);
   for (int c = 0, odd = 0; c < it.n; c += kChunk, odd ^= 1) {
     const int n = min(kChunk, it.n - c);
     const unsigned char* const Lk = L.k[odd];
     u32x4 vf[2][2];  // V^T: [32 tokens][16 columns]
     for (int gq = 0; gq < G; ++gq) {
-      arrived();  // q and k; and the chunk before is done with v
-      if (gq == 0) fetch(L.v, a.v, a.v_stride, h, c);
+      if (gq == 0) arrived_but_v();
+      else arrived();
       // O^T = S^T Q^T and P^T = K Q^T for the chunk's four row tiles.  Lane column m is row i = 16 rt + m; the rows of P^T
       // are keys j = 32 (jt / 2) + 4 (jt % 2) + 8 g + r, and later halves than the row's are left out.
       f32x4 O[4][2] = {}, P[4][4] = {};
@@ -259,12 +262,12 @@ __global__ __launch_bounds__(2 * D, 2) void linear_chunk_kernel(LinearArgs a, Li
       } else {
         fetch(L.q, a.q, a.q_stride, h * G + gq + 1, c);
       }
+      ld_columns<D, 0>(lds_at(L.v), vt_read, vf[0]);
+      ld_columns<D, 1>(lds_at(L.v), vt_read, vf[1]);
       if (!kAttend) break;
       const int es = a.out_f32 ? 4 : 2;
       char* const out = reinterpret_cast<char*>(a.out) + ((it.t0 + (int64_t)c) * a.Hq + h * G + gq) * D * es;
       bool bad = false;
-      ld_columns<D, 0>(lds_at(L.v), vt_read, vf[0]);
-      ld_columns<D, 1>(lds_at(L.v), vt_read, vf[1]);
 #pragma unroll
       for (int rt = 3; rt >= 0; --rt) {
         __builtin_amdgcn_sched_barrier(0);
@@ -348,11 +351,8 @@ __global__ __launch_bounds__(2 * D, 2) void linear_chunk_kernel(LinearArgs a, Li
         }
       }
     }
-    __builtin_amdgcn_sched_barrier(0);
-    if (!kAttend) {
-      ld_columns<D, 0>(lds_at(L.v), vt_read, vf[0]);
-      ld_columns<D, 1>(lds_at(L.v), vt_read, vf[1]);
-    }
+    all_read();
+    fetch(L.v, a.v, a.v_stride, h, c + kChunk);
     const int last = again(n - 1 - 8 * g);
     // S = l^n S + K^T (l^(n-1-j) v_j); rows from n on are zeros
     float keep = L.pw[n + 63];
