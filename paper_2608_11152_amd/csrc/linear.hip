@@ -105,27 +105,16 @@ struct Tiles {
 
 __device__ __forceinline__ u32x4 ld16(const unsigned char* p) { return *reinterpret_cast<const u32x4*>(p); }
 // The LDS's transposing read: of every 16 lanes, lanes 4 r .. 4 r + 3 name 4 elements each of a row r, and lane l gets
-// element l of the 4 rows.  Here the rows are tokens 32 z + 8 g .. + 3 and .. + 7 of the even and of the odd tile of a pair
-// (8 bytes further), so a lane gets operands of 8 tokens.  In assembly, with its wait: before the builtin the compiler
-// waits for all loads to LDS that are under way, whichever tile they go to.
-__device__ __forceinline__ unsigned lds_at(const unsigned char* p) {
-  return (unsigned)(uintptr_t)(__attribute__((address_space(3))) const unsigned char*)p;
+// element l of the 4 rows.  Here the rows are tokens 32 z + 8 g .. + 3 and .. + 7, so a lane gets an operand of 8 tokens.
+__device__ __forceinline__ u32x2 ld_turned(const unsigned char* p) {
+  typedef short i16x4 __attribute__((ext_vector_type(4)));
+  typedef __attribute__((address_space(3))) i16x4 lds4;
+  return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)p));
 }
-template <int D, int Z>
-__device__ __forceinline__ void ld_columns(unsigned tile, int at, u32x4 out[2]) {
-  u32x2 a, b, c, d;
-  asm volatile(
-      "ds_read_b64_tr_b16 %0, %4 offset:%6\n\t"
-      "ds_read_b64_tr_b16 %1, %5 offset:%7\n\t"
-      "ds_read_b64_tr_b16 %2, %4 offset:%8\n\t"
-      "ds_read_b64_tr_b16 %3, %5 offset:%9\n\t"
-      "s_waitcnt lgkmcnt(0)"
-      : "=&v"(a), "=&v"(b), "=&v"(c), "=&v"(d)
-      : "v"(tile + at), "v"(tile + (at ^ 32)), "n"(64 * D * Z), "n"(64 * D * Z + 8 * D), "n"(64 * D * Z + 8),
-        "n"(64 * D * Z + 8 * D + 8)
-      : "memory");
-  out[0] = u32x4{a[0], a[1], b[0], b[1]};
-  out[1] = u32x4{c[0], c[1], d[0], d[1]};
+template <int D>
+__device__ __forceinline__ u32x4 ld_column(const unsigned char* tile, int at, int z) {
+  const u32x2 x = ld_turned(tile + later<D>(at, 0, 0, z)), y = ld_turned(tile + later<D>(at, 1, 0, z));
+  return u32x4{x[0], x[1], y[0], y[1]};
 }
 
 // A wave's share of a tile from memory straight to LDS, 1 KB at a time: with W waves, rows 1024 / (2 D) (w + W j) ..,
@@ -134,11 +123,16 @@ template <int D>
 __device__ __forceinline__ void fetch_tile(unsigned char* tile, const uint16_t* head, int stride, int n, int w, int lane) {
   constexpr int PL = D / 8, RW = 64 / PL;  // lanes of a row, rows of a wave
   const int row = again(RW * w + lane / PL), src = 16 * ((lane % PL) ^ tile_key<D>(row));
-  const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(
-      const_cast<uint16_t*>(head), 0, 2 * ((kChunk - 1) * stride + D), 0x00020000);
+  const uint64_t base = reinterpret_cast<uint64_t>(head);
+  const u32x4 rsrc{(unsigned)base, (unsigned)(base >> 32) & 0xffffu, (unsigned)(2 * ((kChunk - 1) * stride + D)), 0x00020000u};
+  const unsigned dst = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)(tile) + 1024 * w;
+  // In assembly: after the builtin the compiler makes every transposing read wait for all tiles under way.  The kernel
+  // waits itself, at its barriers; loads of the compiler's own are waited for behind these, or with them.  (The wait
+  // states cover m0, and scalar registers that a vector instruction wrote just before.)
   auto put = [&](int j, int from, int uniform) {
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(
-        rsrc, (__attribute__((address_space(3))) void*)(tile + 1024 * w + 32 * D * j), 16, from, uniform, 0, 0);
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+                 :: "s"(__builtin_amdgcn_readfirstlane(dst + 32 * D * j)), "v"(from), "s"(rsrc), "s"(uniform)
+                 : "memory", "m0");
   };
   if (n == kChunk) {
     const int even = 2 * stride * row + src, odd = 2 * stride * row + (src ^ 32);
@@ -174,17 +168,6 @@ __global__ __launch_bounds__(2 * D, kAttend ? 2 : 3) void linear_chunk_kernel(Li
   if (tid < kPwsBase) L.pws[tid] = 0.0f;
 
   const int col = 32 * w + 8 * (m >> 2) + (m & 3);
-  f32x4 S[MT][2] = {};
-  if (it.src != -1) {
-    const float* from = state_at(a, it.src, h, D) + 8 * g * D + col;
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-      for (int nt = 0; nt < 2; ++nt)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) S[mt][nt][r] = from[(32 * (mt >> 1) + 4 * (mt & 1) + r) * D + 4 * nt];
-  }
-
   // The state's decay over a chunk, l^64 rounded to fp32, would be off the same way at every chunk.  `off` is the
   // product of the factors so far over the true one, within a step of fp32 of 1; each factor takes it back.
   const double l64 = power(l1, kChunk), back = 1.0 / l64;
@@ -207,6 +190,19 @@ __global__ __launch_bounds__(2 * D, kAttend ? 2 : 3) void linear_chunk_kernel(Li
   if (kAttend) fetch(L.q, a.q, a.q_stride, h * G, 0);
   fetch(L.k[0], a.k, a.k_stride, h, 0);
   fetch(L.v, a.v, a.v_stride, h, 0);
+  f32x4 S[MT][2] = {};
+  if (it.src != -1) {
+    const float* from = state_at(a, it.src, h, D) + 8 * g * D + col;
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) S[mt][nt][r] = from[(32 * (mt >> 1) + 4 * (mt & 1) + r) * D + 4 * nt];
+  }
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) asm volatile("" : "+v"(S[mt][0]), "+v"(S[mt][1]));  // waits for it here, not in the loop
+
   for (int c = 0, odd = 0; c < it.n; c += kChunk, odd ^= 1) {
     const int n = min(kChunk, it.n - c);
     const unsigned char* const Lk = L.k[odd];
@@ -262,8 +258,10 @@ __global__ __launch_bounds__(2 * D, kAttend ? 2 : 3) void linear_chunk_kernel(Li
       } else {
         fetch(L.q, a.q, a.q_stride, h * G + gq + 1, c);
       }
-      ld_columns<D, 0>(lds_at(L.v), vt_read, vf[0]);
-      ld_columns<D, 1>(lds_at(L.v), vt_read, vf[1]);
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int nt = 0; nt < 2; ++nt) vf[s][nt] = ld_column<D>(L.v + 8 * nt, vt_read, s);
       if (!kAttend) break;
       const int es = a.out_f32 ? 4 : 2;
       char* const out = reinterpret_cast<char*>(a.out) + ((it.t0 + (int64_t)c) * a.Hq + h * G + gq) * D * es;
@@ -353,7 +351,7 @@ __global__ __launch_bounds__(2 * D, kAttend ? 2 : 3) void linear_chunk_kernel(Li
     }
     all_read();
     fetch(L.v, a.v, a.v_stride, h, c + kChunk);
-    const int last = again(n - 1 - 8 * g);
+    const int last = again(n - 1 - 8 * g), k_at = again(kt_read);
     // S = l^n S + K^T (l^(n-1-j) v_j); rows from n on are zeros
     float keep = L.pw[n + 63];
     if (n == kChunk && track) {
@@ -384,9 +382,7 @@ __global__ __launch_bounds__(2 * D, kAttend ? 2 : 3) void linear_chunk_kernel(Li
       // Four independent sums at a time: one product's result is the next but three's summand.
 #pragma unroll
       for (int mt = 0; mt < MT; mt += 2) {
-        u32x4 kf[2];
-        if (s == 0) ld_columns<D, 0>(lds_at(Lk), kt_read ^ (32 * mt), kf);
-        else ld_columns<D, 1>(lds_at(Lk), kt_read ^ (32 * mt), kf);
+        const u32x4 kf[2] = {ld_column<D>(Lk, k_at ^ (32 * mt), s), ld_column<D>(Lk + 8, k_at ^ (32 * mt), s)};
 #pragma unroll
         for (int x = 2; x >= 0; --x)
 #pragma unroll
