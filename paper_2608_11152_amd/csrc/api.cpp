@@ -614,14 +614,14 @@ int check_cu(const int32_t* cu, int num_seqs) {
   return KVP_OK;
 }
 
-// The work of linear_chunk_attn.  Workgroups fit the GPU two to a compute unit; a sequence of more than twice an even
+// The work of linear_chunk_attn.  Workgroups fit the GPU three to a compute unit; a sequence of more than twice an even
 // share of the call's tokens is cut into parts of about that share.
 struct LinearPlan {
   std::vector<kvp::LinearItem> items, sums;
   std::vector<kvp::LinearScan> scans;
   int parts = 0;
 };
-constexpr int kLinearBlocks = 512, kLinearMinPart = 256, kLinearPartStep = 64;
+constexpr int kLinearBlocks = 768, kLinearMinPart = 256, kLinearPartStep = 64;
 
 // src, dst: nullable (only the number of parts is wanted).
 void plan_linear(const int32_t* cu, int num_seqs, int num_kv_heads, const int32_t* src, const int32_t* dst,

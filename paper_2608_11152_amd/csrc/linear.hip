@@ -18,11 +18,9 @@
 //   P^T (keys x rows)   = K Q^T           O^T (columns x rows) = S^T Q^T + V^T P^T           S (dims x columns) = K^T V
 // Rows of q, k and v go from memory straight to LDS; K^T and V^T come from there through its transposing reads.
 //
-// A sequence that would leave compute units without work is cut into parts (plan_linear): linear_chunk_kernel without its
-// outputs sums each part from zeros, linear_scan_kernel turns the sums into the states before the parts, and the parts are
+// A sequence that would leave compute units without work is cut into parts (plan_linear): linear_sum_kernel sums each part
+// from zeros, linear_scan_kernel turns the sums into the states before the parts, and the parts are
 // items.  The parts' keys and values are read twice.
-//
-// Each wave computes all of P^T (a tenth of its matrix work) rather than share it through LDS and a barrier.
 //
 // Operands that are not bf16 are carried as sums of bf16 parts: S and P as two (2^-18 left: far inside a bf16 output's
 // half step 2^-9), the decayed V that goes into the state as three (2^-26: the state is fp32).
@@ -61,12 +59,6 @@ __device__ __forceinline__ unsigned part(float& x, float& y) {
   return w;
 }
 
-// x, as a value that the compiler does not know: reads at it are made again instead of held in registers.
-__device__ __forceinline__ int again(int x) {
-  asm volatile("" : "+v"(x));
-  return x;
-}
-
 __device__ double power(double x, unsigned n) {
   double y = 1.0;
   for (; n; n >>= 1, x *= x)
@@ -95,12 +87,23 @@ __device__ __forceinline__ int later(int at, int y, int x, int z) {
   return (at ^ (32 * (x ^ y))) + 2 * D * (4 * y + 16 * x + 32 * z);
 }
 
+// Row tile rt (16 rows) sees keys of the halves s <= rt / 2 of a chunk.
+__host__ __device__ constexpr int pair_of(int rt, int s) { return rt < 2 ? rt : 2 * rt - 2 + s; }
 constexpr int kPwsBase = 31;
-template <int D, bool kAttend>
+constexpr int kWeights = 6 * 2 * 1024;  // two bf16 parts of 6 operands, 16 bytes a lane
+
+template <int D>
 struct Tiles {
-  unsigned char q[kAttend ? 2 * D * kChunk : 16], k[2][2 * D * kChunk], v[2 * D * kChunk];
-  float pw[2 * kChunk];             // decay^(e - 63), 0 below
+  unsigned char q[2 * D * kChunk > kWeights ? 2 * D * kChunk : kWeights];  // later the weights
+  unsigned char k[2 * D * kChunk], v[2 * D * kChunk];
+  float pw[2 * kChunk];              // decay^(e - 63), 0 below
   float pws[kChunk + 1 + kPwsBase];  // scale decay^(e - kPwsBase), 0 below
+};
+
+template <int D>
+struct SumTiles {
+  unsigned char k[2][2 * D * kChunk], v[2 * D * kChunk];
+  float pw[2 * kChunk];
 };
 
 __device__ __forceinline__ u32x4 ld16(const unsigned char* p) { return *reinterpret_cast<const u32x4*>(p); }
@@ -122,7 +125,7 @@ __device__ __forceinline__ u32x4 ld_column(const unsigned char* tile, int at, in
 template <int D>
 __device__ __forceinline__ void fetch_tile(unsigned char* tile, const uint16_t* head, int stride, int n, int w, int lane) {
   constexpr int PL = D / 8, RW = 64 / PL;  // lanes of a row, rows of a wave
-  const int row = again(RW * w + lane / PL), src = 16 * ((lane % PL) ^ tile_key<D>(row));
+  const int row = RW * w + lane / PL, src = 16 * ((lane % PL) ^ tile_key<D>(row));
   const uint64_t base = reinterpret_cast<uint64_t>(head);
   const u32x4 rsrc{(unsigned)base, (unsigned)(base >> 32) & 0xffffu, (unsigned)(2 * ((kChunk - 1) * stride + D)), 0x00020000u};
   const unsigned dst = (unsigned)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)(tile) + 1024 * w;
@@ -150,145 +153,282 @@ __device__ __forceinline__ float* state_at(const LinearArgs& a, int slot, int h,
   return base + ((int64_t)(slot >= 0 ? slot : -2 - slot) * a.Hkv + h) * D * D;
 }
 
-// kAttend: outputs and state; otherwise only the state, from zeros (the sum of a part of a long sequence).
-template <int D, bool kAttend>
-__global__ __launch_bounds__(2 * D, kAttend ? 2 : 3) void linear_chunk_kernel(LinearArgs a, LinearItems list) {
-  __shared__ Tiles<D, kAttend> L;
-  constexpr int KS = D / 32, MT = D / 16;  // k-steps and row tiles over the dims of k
-  const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, m = lane & 15, g = lane >> 4;
-  const int item = blockIdx.x / a.Hkv, h = blockIdx.x - item * a.Hkv, G = kAttend ? a.Hq / a.Hkv : 1;
-  const LinearItem it = list.items[item];
-  const double l1 = (double)list.decay[h];
+#define KVP_ASM_BARRIER(loads) asm volatile("s_waitcnt vmcnt(" #loads ") lgkmcnt(0)\n\ts_barrier" ::: "memory")
+// Every wave's loads have arrived; all but its last four (one fetch_tile); its LDS reads and writes are done.
+__device__ __forceinline__ void arrived() { KVP_ASM_BARRIER(0); }
+__device__ __forceinline__ void arrived_but_4() { KVP_ASM_BARRIER(4); }
+__device__ __forceinline__ void all_read() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+#undef KVP_ASM_BARRIER
+
+__device__ __forceinline__ double uniform(double x) {  // of a value that all lanes have: in scalar registers
+  const u32x2 u = __builtin_bit_cast(u32x2, x);
+  return __builtin_bit_cast(double, u32x2{(unsigned)__builtin_amdgcn_readfirstlane((int)u[0]),
+                                          (unsigned)__builtin_amdgcn_readfirstlane((int)u[1])});
+}
+
+// A lane's number, asked for again: two instructions instead of registers held through the chunk.
+struct Lane {
+  int lane, m, g;
+  __device__ __forceinline__ Lane() {
+    asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(lane));
+    m = lane & 15;
+    g = lane >> 4;
+  }
+};
+
+// What a wave of a chunk kernel is, and the parts that both kernels share.
+template <int D>
+struct Wave {
+  static constexpr int MT = D / 16;  // row tiles over the dims of k
+  int w, item, h;
+  __device__ __forceinline__ explicit Wave(int Hkv)
+      : w(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)), item(blockIdx.x / Hkv), h(blockIdx.x - item * Hkv) {}
+
+  __device__ __forceinline__ void fetch(unsigned char* tile, const uint16_t* x, int64_t stride, int head, const LinearItem& it,
+                                        int c) const {
+    if (c < it.n)
+      fetch_tile<D>(tile, x + (it.t0 + (int64_t)c) * stride + head * D, (int)stride, min(kChunk, it.n - c), w, Lane().lane);
+  }
+
+  // Rows of a tile that stand in for those behind the item's last: v's must not count.
+  __device__ __forceinline__ void clear_behind(unsigned char* v, int n) const {
+    for (int e = 64 * w + Lane().lane; e < (kChunk - n) * (D / 8); e += 2 * D)
+      *reinterpret_cast<u32x4*>(v + 2 * D * n + 16 * e) = u32x4{0, 0, 0, 0};
+  }
+
+  // The wave's 32 columns of the state: tiles [row tile][column tile], element offsets of a lane's 4 rows.
+  __device__ __forceinline__ int state_lane() const {
+    const Lane l;
+    return 8 * l.g * D + 32 * w + 8 * (l.m >> 2) + (l.m & 3);
+  }
+  __device__ __forceinline__ static constexpr int state_off(int mt, int nt, int r) {
+    return (32 * (mt >> 1) + 4 * (mt & 1) + r) * D + 4 * nt;
+  }
+
+  // V^T: operands of [32 tokens][16 columns]
+  __device__ __forceinline__ void load_v(const unsigned char* v, u32x4 vf[2][2]) const {
+    const Lane l;
+    const int at = tile_at<D>(8 * l.g + (l.m >> 2), 4 * w + (l.m & 3));
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int nt = 0; nt < 2; ++nt) vf[s][nt] = ld_column<D>(v + 8 * nt, at, s);
+  }
+
+  // S = keep S + K^T (l^(n-1-j) v_j); v's rows from n on are zeros
+  __device__ __forceinline__ void update(f32x4 S[MT][2], const unsigned char* k, const u32x4 vf[2][2], const float* pw, int n,
+                                         float keep) const {
+    const Lane l;
+    const int last = n - 1 - 8 * l.g, at = tile_at<D>(8 * l.g + (l.m >> 2), l.m & 3);
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int nt = 0; nt < 2; ++nt) S[mt][nt] *= keep;
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      __builtin_amdgcn_sched_barrier(0);
+      float d[8];
+#pragma unroll
+      for (int b = 0; b < 8; ++b) d[b] = pw[last - (32 * s + b) + 63];
+      u32x4 vp[2][3];
+#pragma unroll
+      for (int nt = 0; nt < 2; ++nt) {
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+          float x = low(vf[s][nt][b]) * d[2 * b], y = high(vf[s][nt][b]) * d[2 * b + 1];
+          vp[nt][0][b] = part(x, y);
+          vp[nt][1][b] = part(x, y);
+          vp[nt][2][b] = pack2(x, y);
+        }
+      }
+      // Four independent sums at a time: one product's result is the next but three's summand.
+#pragma unroll
+      for (int mt = 0; mt < MT; mt += 2) {
+        if (mt % 4 == 0) __builtin_amdgcn_sched_barrier(0);
+        const u32x4 kf[2] = {ld_column<D>(k, at ^ (32 * mt), s), ld_column<D>(k + 8, at ^ (32 * mt), s)};
+#pragma unroll
+        for (int x = 2; x >= 0; --x)
+#pragma unroll
+          for (int y = 0; y < 4; ++y) S[mt + (y >> 1)][y & 1] = mfma16(kf[y >> 1], vp[y & 1][x], S[mt + (y >> 1)][y & 1]);
+      }
+    }
+  }
+};
+
+// The state's decay over a chunk, l^64 rounded to fp32, would be off the same way at every chunk.  `off` is the product of
+// the factors so far over the true one, within a step of fp32 of 1; each factor takes it back.
+struct ChunkDecay {
+  double whole, back, off = 1.0;
+  __device__ __forceinline__ explicit ChunkDecay(double l) : whole(uniform(power(l, kChunk))), back(uniform(1.0 / whole)) {}
+  __device__ __forceinline__ float next(float table, int n) {
+    if (n < kChunk || whole < 1e-30) return table;  // the last chunk; or nothing is left of the state
+    const float f = (float)(whole * (2.0 - off));
+    off = uniform(off * ((double)f * back));
+    return f;
+  }
+};
+
+// The sum of a part of a long sequence: its state from zeros, for linear_scan_kernel.
+template <int D>
+__global__ __launch_bounds__(2 * D, 3) void linear_sum_kernel(LinearArgs a, LinearItems list) {
+  __shared__ SumTiles<D> L;
+  const Wave<D> me(a.Hkv);
+  const LinearItem it = list.sums[me.item];
+  ChunkDecay decay((double)list.decay[me.h]);
+  for (int e = threadIdx.x; e < 2 * kChunk; e += 2 * D)
+    L.pw[e] = e < 63 ? 0.0f : (float)power((double)list.decay[me.h], e - 63);
+  f32x4 S[Wave<D>::MT][2] = {};
+  me.fetch(L.k[0], a.k, a.k_stride, me.h, it, 0);
+  me.fetch(L.v, a.v, a.v_stride, me.h, it, 0);
+  for (int c = 0, odd = 0; c < it.n; c += kChunk, odd ^= 1) {
+    const int n = min(kChunk, it.n - c);
+    arrived();
+    if (n < kChunk) {
+      me.clear_behind(L.v, n);
+      all_read();
+    }
+    me.fetch(L.k[odd ^ 1], a.k, a.k_stride, me.h, it, c + kChunk);
+    u32x4 vf[2][2];
+    me.load_v(L.v, vf);
+    all_read();
+    me.fetch(L.v, a.v, a.v_stride, me.h, it, c + kChunk);
+    me.update(S, L.k[odd], vf, L.pw, n, decay.next(L.pw[n + 63], n));
+  }
+  float* to = state_at(a, it.dst, me.h, D) + me.state_lane();
+#pragma unroll
+  for (int mt = 0; mt < Wave<D>::MT; ++mt)
+#pragma unroll
+    for (int nt = 0; nt < 2; ++nt)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) to[Wave<D>::state_off(mt, nt, r)] = S[mt][nt][r];
+}
+
+template <int D>
+__global__ __launch_bounds__(2 * D, 3) void linear_chunk_kernel(LinearArgs a, LinearItems list) {
+  __shared__ Tiles<D> L;
+  constexpr int KS = D / 32, MT = Wave<D>::MT;  // k-steps and row tiles over the dims of k
+  const Wave<D> me(a.Hkv);
+  const int w = me.w, h = me.h, G = a.Hq / a.Hkv, tid = threadIdx.x;
+  const LinearItem it = list.items[me.item];
+  ChunkDecay decay((double)list.decay[h]);
   if (tid <= kChunk) {
-    const double x = power(l1, tid);
+    const double x = power((double)list.decay[h], tid);
     L.pw[tid + 63] = (float)x;
     L.pws[tid + kPwsBase] = (float)(a.scale * x);
   }
   if (tid < 63) L.pw[tid] = 0.0f;
   if (tid < kPwsBase) L.pws[tid] = 0.0f;
 
-  const int col = 32 * w + 8 * (m >> 2) + (m & 3);
-  // The state's decay over a chunk, l^64 rounded to fp32, would be off the same way at every chunk.  `off` is the
-  // product of the factors so far over the true one, within a step of fp32 of 1; each factor takes it back.
-  const double l64 = power(l1, kChunk), back = 1.0 / l64;
-  const bool track = l64 > 1e-30;
-  double off = 1.0;
-
-  const int q_read = tile_at<D>(m, g), k_read = tile_at<D>(8 * (m >> 2) + (m & 3), g);
-  const int kt_read = tile_at<D>(8 * g + (m >> 2), m & 3), vt_read = tile_at<D>(8 * g + (m >> 2), 4 * w + (m & 3));
-  auto arrived = [&]() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
-  // All loads but the last four, which are v's: fetch_tile is four.
-  auto arrived_but_v = [&]() { asm volatile("s_waitcnt vmcnt(4) lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
-  auto all_read = [&]() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
-  auto fetch = [&](unsigned char* tile, const uint16_t* x, int64_t stride, int head, int c) {
-    if (c < it.n)
-      fetch_tile<D>(tile, x + (it.t0 + (int64_t)c) * stride + head * D, (int)stride, min(kChunk, it.n - c), w, lane);
-  };
-
-  // Loads are under way while there is work that does not need them: the next q and k (which has two places) from the end
-  // of the products with q on, the next v from when the outputs are written until the next products with q are done.
-  if (kAttend) fetch(L.q, a.q, a.q_stride, h * G, 0);
-  fetch(L.k[0], a.k, a.k_stride, h, 0);
-  fetch(L.v, a.v, a.v_stride, h, 0);
+  // Loads are under way while there is work that does not need them: the next q and v during the update of the state, the
+  // next k (its tile is the update's) and still v during the state's product with q.
+  me.fetch(L.q, a.q, a.q_stride, h * G, it, 0);
+  me.fetch(L.v, a.v, a.v_stride, h, it, 0);
   f32x4 S[MT][2] = {};
   if (it.src != -1) {
-    const float* from = state_at(a, it.src, h, D) + 8 * g * D + col;
+    const float* from = state_at(a, it.src, h, D) + me.state_lane();
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
       for (int nt = 0; nt < 2; ++nt)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) S[mt][nt][r] = from[(32 * (mt >> 1) + 4 * (mt & 1) + r) * D + 4 * nt];
+        for (int r = 0; r < 4; ++r) S[mt][nt][r] = from[Wave<D>::state_off(mt, nt, r)];
   }
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) asm volatile("" : "+v"(S[mt][0]), "+v"(S[mt][1]));  // waits for it here, not in the loop
 
-  for (int c = 0, odd = 0; c < it.n; c += kChunk, odd ^= 1) {
+  for (int c = 0; c < it.n; c += kChunk) {
     const int n = min(kChunk, it.n - c);
-    const unsigned char* const Lk = L.k[odd];
-    u32x4 vf[2][2];  // V^T: [32 tokens][16 columns]
+    arrived_but_4();  // q (not yet v); and the update is done with k
+    me.fetch(L.k, a.k, a.k_stride, h, it, c);
+    u32x4 vf[2][2];
     for (int gq = 0; gq < G; ++gq) {
-      if (gq == 0) arrived_but_v();
-      else arrived();
-      // O^T = S^T Q^T and P^T = K Q^T for the chunk's four row tiles.  Lane column m is row i = 16 rt + m; the rows of P^T
-      // are keys j = 32 (jt / 2) + 4 (jt % 2) + 8 g + r, and later halves than the row's are left out.
-      f32x4 O[4][2] = {}, P[4][4] = {};
+      if (gq > 0) arrived();
+      // O^T = S^T Q^T for the chunk's four row tiles, lane column m being row i = 16 rt + m
+      const Lane l0;
+      const int q_at = tile_at<D>(l0.m, l0.g);
+      f32x4 O[4][2] = {};
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt) asm volatile("" : "+v"(S[mt][0]), "+v"(S[mt][1]));  // (not split once for all heads)
-      if (kAttend) {
-        const int q_at = again(q_read), k_at = again(k_read);
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-          __builtin_amdgcn_sched_barrier(0);
-          u32x4 qf[4], kf[4];
+      for (int ks = 0; ks < KS; ++ks) {
+        __builtin_amdgcn_sched_barrier(0);
+        u32x4 qf[4];
 #pragma unroll
-          for (int rt = 0; rt < 4; ++rt) {
-            qf[rt] = ld16(L.q + later<D>(q_at ^ (64 * ks), 0, rt & 1, rt >> 1));
-            kf[rt] = ld16(Lk + later<D>(k_at ^ (64 * ks), rt & 1, 0, rt >> 1));
+        for (int rt = 0; rt < 4; ++rt) qf[rt] = ld16(L.q + later<D>(q_at ^ (64 * ks), 0, rt & 1, rt >> 1));
+#pragma unroll
+        for (int nt = 0; nt < 2; ++nt) {
+          u32x4 hi, lo;
+#pragma unroll
+          for (int b = 0; b < 4; ++b) {
+            float x = S[2 * ks + (b >> 1)][nt][2 * (b & 1)], y = S[2 * ks + (b >> 1)][nt][2 * (b & 1) + 1];
+            hi[b] = part(x, y);
+            lo[b] = pack2(x, y);
           }
 #pragma unroll
-          for (int nt = 0; nt < 2; ++nt) {
-            u32x4 hi, lo;
+          for (int rt = 0; rt < 4; ++rt) O[rt][nt] = mfma16(hi, qf[rt], O[rt][nt]);
 #pragma unroll
-            for (int b = 0; b < 4; ++b) {
-              float x = S[2 * ks + (b >> 1)][nt][2 * (b & 1)], y = S[2 * ks + (b >> 1)][nt][2 * (b & 1) + 1];
-              hi[b] = part(x, y);
-              lo[b] = pack2(x, y);
-            }
-#pragma unroll
-            for (int rt = 0; rt < 4; ++rt) O[rt][nt] = mfma16(hi, qf[rt], O[rt][nt]);
-#pragma unroll
-            for (int rt = 0; rt < 4; ++rt) O[rt][nt] = mfma16(lo, qf[rt], O[rt][nt]);
-          }
-#pragma unroll
-          for (int rt = 0; rt < 4; ++rt)
-#pragma unroll
-            for (int jt = 0; jt < 2 * (rt / 2) + 2; ++jt) P[rt][jt] = mfma16(kf[jt], qf[rt], P[rt][jt]);
+          for (int rt = 0; rt < 4; ++rt) O[rt][nt] = mfma16(lo, qf[rt], O[rt][nt]);
         }
       }
-      arrived();  // v; and q has been read
-      if (gq == 0 && n < kChunk) {  // the rows that stand in for those behind the last: v must not count
-        for (int e = tid; e < (kChunk - n) * (D / 8); e += 2 * D)
-          *reinterpret_cast<u32x4*>(L.v + 2 * D * n + 16 * e) = u32x4{0, 0, 0, 0};
-        all_read();
+      __builtin_amdgcn_sched_barrier(0);
+      if (gq == 0) {
+        arrived();  // k and v
+        if (n < kChunk) me.clear_behind(L.v, n);  // (before the next barrier but one, after which v is read)
       }
-      if (gq == G - 1) {
-        if (kAttend) fetch(L.q, a.q, a.q_stride, h * G, c + kChunk);
-        fetch(L.k[odd ^ 1], a.k, a.k_stride, h, c + kChunk);
-      } else {
-        fetch(L.q, a.q, a.q_stride, h * G + gq + 1, c);
+      // The wave's share of the tiles (rt, jt) of P^T = K Q^T; its rows are keys j = 32 (jt / 2) + 4 (jt % 2) + 8 g + r.
+      constexpr int W = D / 32, N = 12 / W;
+      u32x2 weight[N][2];
+      {
+        const Lane l;
+        const int k_at = tile_at<D>(8 * (l.m >> 2) + (l.m & 3), l.g), q_at = tile_at<D>(l.m, l.g);
+        f32x4 P[N] = {};
+        int qa[N], ka[N];
+#pragma unroll
+        for (int x = 0; x < N; ++x) {
+          const int t = w + W * x, rt = t < 4 ? t >> 1 : 2 + ((t - 4) >> 2), jt = t < 4 ? t & 1 : t & 3;
+          qa[x] = later<D>(q_at, 0, rt & 1, rt >> 1);
+          ka[x] = later<D>(k_at, jt & 1, 0, jt >> 1);
+        }
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+          for (int x = 0; x < N; ++x) P[x] = mfma16(ld16(L.k + (ka[x] ^ (64 * ks))), ld16(L.q + (qa[x] ^ (64 * ks))), P[x]);
+#pragma unroll
+        for (int x = 0; x < N; ++x) {
+          const int t = w + W * x, rt = t < 4 ? t >> 1 : 2 + ((t - 4) >> 2), jt = t < 4 ? t & 1 : t & 3;
+          const int e = l.m - 8 * l.g + 16 * rt - 32 * (jt >> 1) - 4 * (jt & 1);  // i - j for r = 0
+#pragma unroll
+          for (int r = 0; r < 4; ++r) P[x][r] = e - r >= 0 ? P[x][r] * L.pws[e - r + kPwsBase] : 0.0f;
+#pragma unroll
+          for (int b = 0; b < 2; ++b) {
+            float y0 = P[x][2 * b], y1 = P[x][2 * b + 1];
+            weight[x][0][b] = part(y0, y1);
+            weight[x][1][b] = pack2(y0, y1);
+          }
+        }
       }
+      all_read();  // q, whose place the weights take: by pair_of, part and lane
 #pragma unroll
-      for (int s = 0; s < 2; ++s)
-#pragma unroll
-        for (int nt = 0; nt < 2; ++nt) vf[s][nt] = ld_column<D>(L.v + 8 * nt, vt_read, s);
-      if (!kAttend) break;
+      for (int x = 0; x < N; ++x) {
+        const int t = w + W * x, rt = t < 4 ? t >> 1 : 2 + ((t - 4) >> 2), jt = t < 4 ? t & 1 : t & 3;
+        unsigned char* const to = L.q + 2048 * pair_of(rt, jt >> 1) + 16 * Lane().lane + 8 * (jt & 1);
+        *reinterpret_cast<u32x2*>(to) = weight[x][0];
+        *reinterpret_cast<u32x2*>(to + 1024) = weight[x][1];
+      }
+      all_read();
+      me.load_v(L.v, vf);
       const int es = a.out_f32 ? 4 : 2;
       char* const out = reinterpret_cast<char*>(a.out) + ((it.t0 + (int64_t)c) * a.Hq + h * G + gq) * D * es;
       bool bad = false;
 #pragma unroll
       for (int rt = 3; rt >= 0; --rt) {
         __builtin_amdgcn_sched_barrier(0);
-        const int mg = again(m - 8 * g);
-#pragma unroll
-        for (int jt = 0; jt < 2 * (rt / 2) + 2; ++jt)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const bool whole = jt / 2 < rt / 2;  // all of these keys are before all of the rows
-            const int e = mg + 16 * rt - 32 * (jt >> 1) - 4 * (jt & 1) - r;
-            P[rt][jt][r] *= L.pws[e + kPwsBase];
-            if (!whole && e < 0) P[rt][jt][r] = 0.0f;
-          }
+        const Lane l;
         f32x4 V[2] = {};
 #pragma unroll
         for (int s = 0; s <= rt / 2; ++s) {
-          u32x4 hi, lo;
-#pragma unroll
-          for (int b = 0; b < 4; ++b) {
-            float x = P[rt][2 * s + (b >> 1)][2 * (b & 1)], y = P[rt][2 * s + (b >> 1)][2 * (b & 1) + 1];
-            hi[b] = part(x, y);
-            lo[b] = pack2(x, y);
-          }
+          const unsigned char* const from = L.q + 2048 * pair_of(rt, s) + 16 * l.lane;
+          const u32x4 hi = ld16(from), lo = ld16(from + 1024);
 #pragma unroll
           for (int nt = 0; nt < 2; ++nt) V[nt] = mfma16(vf[s][nt], hi, V[nt]);
 #pragma unroll
@@ -304,14 +444,14 @@ __global__ __launch_bounds__(2 * D, kAttend ? 2 : 3) void linear_chunk_kernel(Li
             float y = 0.0f;
 #pragma unroll 1
             for (int s = 0; s < 4; ++s) {
-              const u32x4 v = ld16(L.v + tile_at<D>(lane, 4 * w + s));
+              const u32x4 v = ld16(L.v + tile_at<D>(l.lane, 4 * w + s));
 #pragma unroll
               for (int b = 0; b < 4; ++b) y += (low(v[b]) - low(v[b])) + (high(v[b]) - high(v[b]));
             }
             bad = __any(y != 0.0f);
           }
         }
-        const int i = 16 * rt + m;
+        const int i = 16 * rt + l.m;
         if (bad) {  // key by key: only keys up to the row are multiplied at all
           const uint16_t* const qi = a.q + (it.t0 + (int64_t)(c + min(i, n - 1))) * a.q_stride + (h * G + gq) * D;
           V[0] = V[1] = f32x4{};
@@ -320,24 +460,24 @@ __global__ __launch_bounds__(2 * D, kAttend ? 2 : 3) void linear_chunk_kernel(Li
             float p = 0.0f;
 #pragma unroll 1
             for (int d = 0; d < D / 8; ++d) {
-              const u32x4 x = *reinterpret_cast<const u32x4*>(qi + 8 * d), y = ld16(Lk + tile_at<D>(j, d));
+              const u32x4 x = *reinterpret_cast<const u32x4*>(qi + 8 * d), y = ld16(L.k + tile_at<D>(j, d));
 #pragma unroll
               for (int b = 0; b < 4; ++b) p = fmaf(high(x[b]), high(y[b]), fmaf(low(x[b]), low(y[b]), p));
             }
-            p *= L.pws[i - j + kPwsBase > 0 ? i - j + kPwsBase : 0];
-            const u32x4 v = ld16(L.v + tile_at<D>(j, 4 * w + g));
+            p *= L.pws[max(i - j, 0) + kPwsBase];
+            const u32x4 v = ld16(L.v + tile_at<D>(j, 4 * w + l.g));
 #pragma unroll
             for (int x = 0; x < 8; ++x)
               if (j <= i) V[x >> 2][x & 3] = fmaf(p, x & 1 ? high(v[x >> 1]) : low(v[x >> 1]), V[x >> 2][x & 3]);
           }
         }
-        const float f = L.pws[again(i + 1) + kPwsBase];
+        const float f = L.pws[i + 1 + kPwsBase];
 #pragma unroll
         for (int nt = 0; nt < 2; ++nt)
 #pragma unroll
           for (int r = 0; r < 4; ++r) V[nt][r] = fmaf(O[rt][nt][r], f, V[nt][r]);
         if (i < n) {
-          const int at = again(i) * a.Hq * D + 32 * w + 8 * g;
+          const int at = i * a.Hq * D + 32 * w + 8 * l.g;
           if (a.out_f32) {
             f32x4* o = reinterpret_cast<f32x4*>(out + 4 * (int64_t)at);
             o[0] = V[0];
@@ -348,56 +488,21 @@ __global__ __launch_bounds__(2 * D, kAttend ? 2 : 3) void linear_chunk_kernel(Li
           }
         }
       }
+      all_read();  // the weights and v
+      if (gq + 1 < G) me.fetch(L.q, a.q, a.q_stride, h * G + gq + 1, it, c);
     }
-    all_read();
-    fetch(L.v, a.v, a.v_stride, h, c + kChunk);
-    const int last = again(n - 1 - 8 * g), k_at = again(kt_read);
-    // S = l^n S + K^T (l^(n-1-j) v_j); rows from n on are zeros
-    float keep = L.pw[n + 63];
-    if (n == kChunk && track) {
-      keep = (float)(l64 * (2.0 - off));
-      off *= (double)keep * back;
-    }
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-      for (int nt = 0; nt < 2; ++nt) S[mt][nt] *= keep;
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      __builtin_amdgcn_sched_barrier(0);
-      float d[8];
-#pragma unroll
-      for (int b = 0; b < 8; ++b) d[b] = L.pw[last - (32 * s + b) + 63];
-      u32x4 vp[2][3];
-#pragma unroll
-      for (int nt = 0; nt < 2; ++nt) {
-#pragma unroll
-        for (int b = 0; b < 4; ++b) {
-          float x = low(vf[s][nt][b]) * d[2 * b], y = high(vf[s][nt][b]) * d[2 * b + 1];
-          vp[nt][0][b] = part(x, y);
-          vp[nt][1][b] = part(x, y);
-          vp[nt][2][b] = pack2(x, y);
-        }
-      }
-      // Four independent sums at a time: one product's result is the next but three's summand.
-#pragma unroll
-      for (int mt = 0; mt < MT; mt += 2) {
-        const u32x4 kf[2] = {ld_column<D>(Lk, k_at ^ (32 * mt), s), ld_column<D>(Lk + 8, k_at ^ (32 * mt), s)};
-#pragma unroll
-        for (int x = 2; x >= 0; --x)
-#pragma unroll
-          for (int y = 0; y < 4; ++y) S[mt + (y >> 1)][y & 1] = mfma16(kf[y >> 1], vp[y & 1][x], S[mt + (y >> 1)][y & 1]);
-      }
-    }
+    me.fetch(L.q, a.q, a.q_stride, h * G, it, c + kChunk);
+    me.fetch(L.v, a.v, a.v_stride, h, it, c + kChunk);
+    me.update(S, L.k, vf, L.pw, n, decay.next(L.pw[n + 63], n));
   }
   if (it.dst == -1) return;
-  float* to = state_at(a, it.dst, h, D) + 8 * g * D + col;
+  float* to = state_at(a, it.dst, h, D) + me.state_lane();
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
     for (int nt = 0; nt < 2; ++nt)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) to[(32 * (mt >> 1) + 4 * (mt & 1) + r) * D + 4 * nt] = S[mt][nt][r];
+      for (int r = 0; r < 4; ++r) to[Wave<D>::state_off(mt, nt, r)] = S[mt][nt][r];
 }
 
 // States before each part of the long sequences, from the parts' own sums: S_0 = source, S_i = l^len S_(i-1) + sum_(i-1).
@@ -504,12 +609,10 @@ hipError_t launch_linear_decode(const LinearArgs& a, const LinearBatch& batch, i
 template <int D>
 static void launch_chunk(const LinearArgs& a, const LinearItems& list, hipStream_t s) {
   if (list.n_scans > 0) {
-    LinearItems sums = list;
-    sums.items = list.sums;
-    hipLaunchKernelGGL((linear_chunk_kernel<D, false>), dim3(list.n_sums * a.Hkv), dim3(2 * D), 0, s, a, sums);
+    hipLaunchKernelGGL(linear_sum_kernel<D>, dim3(list.n_sums * a.Hkv), dim3(2 * D), 0, s, a, list);
     hipLaunchKernelGGL(linear_scan_kernel, dim3(list.n_scans * a.Hkv * (D * D / 256)), dim3(256), 0, s, a, list, D);
   }
-  hipLaunchKernelGGL((linear_chunk_kernel<D, true>), dim3(list.n_items * a.Hkv), dim3(2 * D), 0, s, a, list);
+  hipLaunchKernelGGL(linear_chunk_kernel<D>, dim3(list.n_items * a.Hkv), dim3(2 * D), 0, s, a, list);
 }
 
 hipError_t launch_linear_chunk(const LinearArgs& a, const LinearItems& list, int D, hipStream_t s) {
