@@ -133,8 +133,8 @@ __device__ __forceinline__ void fetch_tile(unsigned char* tile, const uint16_t* 
   // waits itself, at its barriers; loads of the compiler's own are waited for behind these, or with them.  (The wait
   // states cover m0, and scalar registers that a vector instruction wrote just before.)
   auto put = [&](int j, int from, int uniform) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
-                 :: "s"(__builtin_amdgcn_readfirstlane(dst + 32 * D * j)), "v"(from), "s"(rsrc), "s"(uniform)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, %3 offen nt lds"
+                 :: "s"(__builtin_amdgcn_readfirstlane(dst + 32 * D * j)), "v"(from), "s"(rsrc), "s"(__builtin_amdgcn_readfirstlane(uniform))
                  : "memory", "m0");
   };
   if (n == kChunk) {
