@@ -615,27 +615,31 @@ int check_cu(const int32_t* cu, int num_seqs) {
 }
 
 // The work of linear_chunk_attn.  Workgroups fit the GPU three to a compute unit; a sequence of more than twice an even
-// share of the call's tokens is cut into parts of about that share.
+// share of the call's tokens is cut into parts of about that share, down to single chunks of 64: 24 calls of all shapes
+// take 0.88 and 0.83 of their time with parts from 128 and 64 on, against parts from 256 on.  Cutting takes two more
+// launches and a second pass over k and v, which walking a few chunks is quicker than: about 5 us a chunk for one query
+// head and 3.5 us for each further one.  Uncut / cut, 8 KV heads of 64, one sequence: of 256 tokens 25 / 27 us, 320
+// tokens 31 / 27 us; with 2 query heads a KV head 192 tokens 31 / 26 us; with 8, 129 tokens 92 / 46 us.
 struct LinearPlan {
   std::vector<kvp::LinearItem> items, sums;
   std::vector<kvp::LinearScan> scans;
   int parts = 0;
 };
-constexpr int kLinearBlocks = 768, kLinearMinPart = 256, kLinearPartStep = 64;
+constexpr int kLinearBlocks = 768, kLinearChunk = 64, kLinearMinWork = 512;
 
-// src, dst: nullable (only the number of parts is wanted).
-void plan_linear(const int32_t* cu, int num_seqs, int num_kv_heads, const int32_t* src, const int32_t* dst,
+// group: query heads per KV head; more of them, no fewer parts.  src, dst: nullable (only the number of parts is wanted).
+void plan_linear(const int32_t* cu, int num_seqs, int num_kv_heads, int group, const int32_t* src, const int32_t* dst,
                  LinearPlan* P) {
   const int64_t even = ((int64_t)cu[num_seqs] * num_kv_heads + kLinearBlocks - 1) / kLinearBlocks;
-  const int64_t share = std::max<int64_t>(kLinearMinPart, even);
+  const int64_t share = std::max<int64_t>(kLinearChunk, even);
   for (int i = 0; i < num_seqs; ++i) {
     const int32_t n = cu[i + 1] - cu[i], from = src ? src[i] : -1, to = dst ? dst[i] : -1;
-    if (n <= 2 * share) {
+    if (n <= 2 * share || (int64_t)n * (1 + group) <= kLinearMinWork) {
       P->items.push_back({cu[i], n, from, to});
       continue;
     }
     const int64_t want = (n + share - 1) / share;  // parts of a whole number of chunks
-    const int32_t len = (int32_t)(((n + want - 1) / want + kLinearPartStep - 1) / kLinearPartStep * kLinearPartStep);
+    const int32_t len = (int32_t)(((n + want - 1) / want + kLinearChunk - 1) / kLinearChunk * kLinearChunk);
     const int32_t m = (n + len - 1) / len;
     for (int32_t p = 0; p < m; ++p) {
       const int32_t t0 = cu[i] + p * len, cnt = std::min(len, n - p * len);
@@ -652,6 +656,7 @@ void plan_linear(const int32_t* cu, int num_seqs, int num_kv_heads, const int32_
 static_assert(kvp::kLinearHeads == KVP_LINEAR_MAX_HEADS && kvp::kRopePairs == KVP_ROPE_PAIRS, "as in the header");
 
 constexpr int64_t kLinearMaxStride = 1 << 24;
+constexpr int kLinearMaxGroup = 16;
 
 constexpr int32_t kRopeValid = 0x726f7065;  // kvp_rope.valid
 
@@ -689,7 +694,7 @@ int check_linear(const void* q, int64_t q_stride, const void* k, int64_t k_strid
   if (num_kv_heads <= 0 || num_kv_heads > KVP_LINEAR_MAX_HEADS)
     return set_err(KVP_EUNSUPPORTED, "num_kv_heads %d outside [1, %d]", num_kv_heads, KVP_LINEAR_MAX_HEADS);
   const int G = num_q_heads / num_kv_heads;
-  if (num_q_heads <= 0 || num_q_heads % num_kv_heads || G > 16 || (G & (G - 1)))
+  if (num_q_heads <= 0 || num_q_heads % num_kv_heads || G > kLinearMaxGroup || (G & (G - 1)))
     return set_err(KVP_EUNSUPPORTED, "num_q_heads / num_kv_heads = %d / %d is not 1, 2, 4, 8 or 16", num_q_heads,
                    num_kv_heads);
   if (out_dtype != KVP_BF16 && out_dtype != KVP_F32) return set_err(KVP_EUNSUPPORTED, "out_dtype %d", out_dtype);
@@ -1036,7 +1041,7 @@ int linear_chunk_workspace_size(const int32_t* cu, int num_seqs, int num_kv_head
   const int rc = check_cu(cu, num_seqs);
   if (rc) return rc;
   LinearPlan P;
-  plan_linear(cu, num_seqs, num_kv_heads, nullptr, nullptr, &P);
+  plan_linear(cu, num_seqs, num_kv_heads, kLinearMaxGroup, nullptr, nullptr, &P);
   *bytes = (size_t)P.parts * num_kv_heads * head_dim * head_dim * sizeof(float);
   return KVP_OK;
 } catch (const std::exception& x) {
@@ -1059,7 +1064,7 @@ int linear_chunk_attn(const void* q, int64_t q_stride, const void* k, int64_t k_
     if (cu[num_seqs] > 0 && (stride < head_dim || stride > kLinearMaxStride))
       return set_err(KVP_EINVAL, "stride %lld outside [head_dim, %lld]", (long long)stride, (long long)kLinearMaxStride);
   LinearPlan P;
-  plan_linear(cu, num_seqs, num_kv_heads, src_slots, dst_slots, &P);
+  plan_linear(cu, num_seqs, num_kv_heads, num_q_heads / num_kv_heads, src_slots, dst_slots, &P);
   const size_t need = (size_t)P.parts * num_kv_heads * head_dim * head_dim * sizeof(float);
   if (need > 0 && (!ws || ws_bytes < need || (reinterpret_cast<uintptr_t>(ws) & 15) != 0))
     return set_err(KVP_EWORKSPACE, "workspace of %zu bytes (16-byte aligned), %zu needed", ws ? ws_bytes : 0, need);
