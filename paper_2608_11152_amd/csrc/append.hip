@@ -81,20 +81,16 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a) {
 
 // ---------------------------------------------------------------------------------------------------
 // FP8 (OCP E4M3) pools: y = fp32(x) * inv_scale is rounded to the nearest E4M3 value, ties to the even
-// mantissa, saturating at +-448; NaN stays NaN.  Integer arithmetic on the binary32 bits.
+// mantissa, saturating at +-448; NaN stays NaN and keeps its sign.  The conversion instruction rounds so;
+// it does not saturate, and sets the sign of every NaN.
 // ---------------------------------------------------------------------------------------------------
-__device__ __forceinline__ unsigned e4m3_code(float y) {
-  const unsigned u = __float_as_uint(y);
-  const unsigned sign = (u >> 24) & 0x80u;
-  const unsigned a = u & 0x7FFFFFFFu;
-  if (a > 0x7F800000u) return sign | 0x7Fu;             // NaN
-  if (a >= 0x43E00000u) return sign | 0x7Eu;            // |y| >= 448 (and infinity): saturate
-  if (a >= 0x3C800000u) {                               // |y| >= 2^-6: normal, keep 3 mantissa bits
-    const unsigned r = a + 0x7FFFFu + ((a >> 20) & 1u);  // round to nearest even at bit 20
-    return sign | ((r >> 20) - ((127u - 7u) << 3));
-  }
-  return sign | (unsigned)__builtin_rintf(__uint_as_float(a) * 512.0f);  // subnormal: m * 2^-9, m <= 8
+__device__ __forceinline__ unsigned e4m3_pair(float x, float y) {  // codes of x and y in the low two bytes
+  const float a = x != x ? x : __builtin_amdgcn_fmed3f(x, -448.0f, 448.0f);
+  const float b = y != y ? y : __builtin_amdgcn_fmed3f(y, -448.0f, 448.0f);
+  const unsigned sign = __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x0c0c0703u);  // their top bytes
+  return ((unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false) & 0x7f7fu) | (sign & 0x8080u);
 }
+__device__ __forceinline__ unsigned e4m3_code(float y) { return e4m3_pair(y, y) & 0xffu; }
 
 __device__ __forceinline__ float bf16_to_f32(uint16_t b) { return __uint_as_float((unsigned)b << 16); }
 
@@ -103,7 +99,8 @@ __device__ __forceinline__ uint2 quant8(uint4 x, float inv) {
   const uint16_t* h = reinterpret_cast<const uint16_t*>(&x);
   unsigned w[2] = {0u, 0u};
 #pragma unroll
-  for (int j = 0; j < 8; ++j) w[j >> 2] |= e4m3_code(bf16_to_f32(h[j]) * inv) << (8 * (j & 3));
+  for (int j = 0; j < 8; j += 2)
+    w[j >> 2] |= e4m3_pair(bf16_to_f32(h[j]) * inv, bf16_to_f32(h[j + 1]) * inv) << (8 * (j & 3));
   return make_uint2(w[0], w[1]);
 }
 
@@ -124,10 +121,11 @@ __device__ __forceinline__ void put_v_fp8(const PageRun& r, const uint16_t* vs, 
     union { uint4 u; uint8_t b[16]; } val;
     if (!all) val.u = *reinterpret_cast<const uint4*>(dst);
     for (int dh = 0; dh < 2; ++dh)
-      for (int j = 0; j < 8; ++j) {
-        const int t = slot_token(8 * h + j);
-        if (t >= r.s_lo && t < r.s_hi)
-          val.b[dh * 8 + j] = (uint8_t)e4m3_code(bf16_to_f32(vs[t * D + 32 * Y + 16 * dh + cc]) * inv_scale);
+      for (int j = 0; j < 8; j += 2) {
+        const int dim = 32 * Y + 16 * dh + cc, t0 = slot_token(8 * h + j), t1 = slot_token(8 * h + j + 1);
+        const unsigned codes = e4m3_pair(bf16_to_f32(vs[t0 * D + dim]) * inv_scale, bf16_to_f32(vs[t1 * D + dim]) * inv_scale);
+        if (t0 >= r.s_lo && t0 < r.s_hi) val.b[dh * 8 + j] = (uint8_t)codes;
+        if (t1 >= r.s_lo && t1 < r.s_hi) val.b[dh * 8 + j + 1] = (uint8_t)(codes >> 8);
       }
     store_stream(reinterpret_cast<uint16_t*>(dst), val.u);
   }
@@ -264,34 +262,41 @@ __global__ __launch_bounds__(256) void append_rope_kernel(AppendRopeArgs r) {
   __shared__ uint16_t vstage[4][16 * D];
   const AppendArgs& a = r.kv;
   const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const unsigned unit = blockIdx.x * 4u + w, run = r.by_slots.quotient(unit);
-  const int slot = (int)(unit - run * r.by_slots.d);
+  // The waves for queries first, then those for keys: taken in turn, workgroups of one kind met on every other XCD.
+  unsigned unit = blockIdx.x * 4u + w;
+  const bool key = unit >= r.q_units;
+  if (key) unit -= r.q_units;
+  const FastDiv& by = key ? r.by_keys : r.by_queries;
+  const unsigned run = by.quotient(unit);
+  const int slot = (int)(unit - run * by.d);
   if (run >= (unsigned)a.n_runs) return;
   const PageRun pr = a.runs[run];
   const int ntok = pr.s_hi - pr.s_lo;
-  const int R = r.table.rotary_dim, turned = IL ? R / 8 : R / 16, units = turned + (D - R) / 8;
+  // Units of a token and head: 8 dims; in the half layout 8 and 8 more, `next` further.
+  constexpr int units = IL ? D / 8 : D / 16;
+  const int R = r.table.rotary_dim, turned = IL ? R / 8 : R / 16;
   const int width = ntok * units > 32 ? 64 : ntok * units > 16 ? 32 : ntok * units > 8 ? 16 : 8;
 
-  if (slot >= a.Hkv) {
-    const int h_lo = (slot - a.Hkv) * kQueryHeads, h_hi = min(h_lo + kQueryHeads, r.Hq);
+  if (!key) {
+    const int h_lo = slot * kQueryHeads, h_hi = min(h_lo + kQueryHeads, r.Hq);
     const int across = 64 / width;  // heads at a time
     for (int e = lane & (width - 1); e < ntok * units; e += width) {
-      const int tt = e / units, u = e - tt * units;
+      const int tt = e / units, u = e % units;
       const int64_t tok = pr.src0 + tt;
       const bool pass = u >= turned;
-      const int i0 = pass ? R + (u - turned) * 8 : u * 8;
+      const int i0 = IL ? 8 * u : pass ? 16 * u : 8 * u, next = pass ? 8 : R / 2;
       const uint16_t* x = r.q + tok * r.q_stride + i0;
       uint16_t* y = r.q_out + tok * r.q_out_stride + i0;
       Turns<IL ? 4 : 8> t;
       if (!pass) t.set(r.table, IL ? u * 4 : u * 8, pr.lpage * 16 + pr.s_lo + tt);
-      constexpr int N = 4;  // heads whose loads are under way together
+      constexpr int N = 2;  // heads whose loads are under way together
       for (int h = h_lo + lane / width; h < h_hi; h += N * across) {
         Eight p[N], q[N];
 #pragma unroll
         for (int n = 0; n < N; ++n)
           if (h + n * across < h_hi) {
             p[n].load(x + (h + n * across) * D);
-            if (!IL && !pass) q[n].load(x + (h + n * across) * D + R / 2);
+            if (!IL) q[n].load(x + (h + n * across) * D + next);
           }
 #pragma unroll
         for (int n = 0; n < N; ++n)
@@ -301,7 +306,7 @@ __global__ __launch_bounds__(256) void append_rope_kernel(AppendRopeArgs r) {
               else turn_halves(p[n], q[n], t);
             }
             p[n].store(y + (h + n * across) * D);
-            if (!IL && !pass) q[n].store(y + (h + n * across) * D + R / 2);
+            if (!IL) q[n].store(y + (h + n * across) * D + next);
           }
       }
     }
@@ -320,7 +325,8 @@ __global__ __launch_bounds__(256) void append_rope_kernel(AppendRopeArgs r) {
     if (F8) {
       unsigned code[2] = {0u, 0u};
 #pragma unroll
-      for (int j = 0; j < 8; ++j) code[j >> 2] |= e4m3_code(v.x[j] * a.inv_scale_k) << (8 * (j & 3));
+      for (int j = 0; j < 8; j += 2)
+        code[j >> 2] |= e4m3_pair(v.x[j] * a.inv_scale_k, v.x[j + 1] * a.inv_scale_k) << (8 * (j & 3));
       *reinterpret_cast<uint2*>(b8 + k8_index<D>(s, c)) = make_uint2(code[0], code[1]);
     } else {
       store_stream(b16 + k_index<D>(s, c), v.bf16());
@@ -334,13 +340,13 @@ __global__ __launch_bounds__(256) void append_rope_kernel(AppendRopeArgs r) {
         *reinterpret_cast<const uint4*>(a.v + (pr.src0 + tt) * r.v_stride + slot * D + c8 * 8);
   }
   for (int e = lane; e < ntok * units; e += 64) {
-    const int tt = e / units, u = e - tt * units, s = pr.s_lo + tt;
+    const int tt = e / units, u = e % units, s = pr.s_lo + tt;
     const uint16_t* x = a.k + (pr.src0 + tt) * r.k_stride + slot * D;
     const bool pass = u >= turned;
-    const int i0 = pass ? R + (u - turned) * 8 : u * 8;
+    const int i0 = IL ? 8 * u : pass ? 16 * u : 8 * u, next = pass ? 8 : R / 2;
     Eight p, q;
     p.load(x + i0);
-    if (!IL && !pass) q.load(x + i0 + R / 2);
+    if (!IL) q.load(x + i0 + next);
     if (!pass) {
       Turns<IL ? 4 : 8> t;
       t.set(r.table, IL ? u * 4 : u * 8, pr.lpage * 16 + s);
@@ -348,7 +354,7 @@ __global__ __launch_bounds__(256) void append_rope_kernel(AppendRopeArgs r) {
       else turn_halves(p, q, t);
     }
     put_k(s, i0, p);
-    if (!IL && !pass) put_k(s, i0 + R / 2, q);
+    if (!IL) put_k(s, i0 + next, q);
   }
   __builtin_amdgcn_wave_barrier();
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
@@ -451,13 +457,16 @@ hipError_t launch_append(const AppendArgs& a, int D, hipStream_t s) {
 template <int D, bool F8>
 static void launch_append_rope(const AppendRopeArgs& a, hipStream_t s) {
   const bool whole = a.table.rotary_dim % (a.table.interleaved ? 8 : 16) == 0;
-  const int slots = a.kv.Hkv + (whole ? (a.Hq + kQueryHeads - 1) / kQueryHeads : a.Hq);
+  const int q_slots = whole ? (a.Hq + kQueryHeads - 1) / kQueryHeads : a.Hq, slots = a.kv.Hkv + q_slots;
   const int most = (int)((1u << 30) / slots);  // runs of a launch: 31-bit unit indices
   AppendRopeArgs b = a;
   b.by_slots = FastDiv(slots);
+  b.by_keys = FastDiv(a.kv.Hkv);
+  b.by_queries = FastDiv(std::max(1, q_slots));
   for (int r = 0; r < a.kv.n_runs; r += most) {
     b.kv.runs = a.kv.runs + r;
     b.kv.n_runs = std::min(most, a.kv.n_runs - r);
+    b.q_units = (unsigned)b.kv.n_runs * q_slots;
     const dim3 grid((unsigned)(((int64_t)b.kv.n_runs * slots + 3) / 4));
     if (!whole) hipLaunchKernelGGL((append_rope_pair_kernel<D, F8>), grid, dim3(256), 0, s, b);
     else if (a.table.interleaved) hipLaunchKernelGGL((append_rope_kernel<D, F8, true>), grid, dim3(256), 0, s, b);

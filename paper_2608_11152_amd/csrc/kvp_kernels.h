@@ -75,7 +75,8 @@ struct AppendRopeArgs {
   uint16_t* q_out;
   int64_t q_stride, q_out_stride;
   int Hq;
-  FastDiv by_slots;         // of a wave's index (set by launch_append_rope)
+  FastDiv by_slots, by_keys, by_queries;  // of a wave's index (these and q_units: set by launch_append_rope)
+  uint32_t q_units;         // waves for queries
 };
 
 // Linear attention over states [slots, Hkv, D, D].  One item is a run of tokens of one sequence.
