@@ -472,17 +472,20 @@ def linear_chunk_attn(q, k, v, state, decay, src_slots, dst_slots, cu, scale=Non
     multiple of 8 elements), state device fp32 [slots, Hkv, d, d]; decay, src_slots, dst_slots, cu host."""
     import torch
     cu = _i32(cu)
-    if len(cu) != len(_i32(src_slots)) + 1:
-        raise ValueError(f"cu has {len(cu)} entries, {len(_i32(src_slots)) + 1} needed")
+    if len(cu) != len(src_slots) + 1:
+        raise ValueError(f"cu has {len(cu)} entries, {len(src_slots) + 1} needed")
     head, tail, out, keep = _linear_args(q, k, v, state, decay, src_slots, dst_slots, int(cu[-1]), scale, out, out_dtype,
                                          stream)
-    if ws is None:
-        n = linear_chunk_workspace_size(cu, k.shape[1], k.shape[2])
-        ws = _alloc_on(stream, n, torch.uint8, q.device) if n else None
+    addr, s = _addr(cu), _stream(stream)
+    if ws is None:  # most calls need none: the size is asked for when the call says so (it has enqueued nothing then)
+        rc = lib().linear_chunk_attn(*head, addr, *tail, None, 0, s)
+        if rc != KVP_EWORKSPACE:
+            _check(rc, "linear_chunk_attn")
+            return out
+        ws = _alloc_on(stream, linear_chunk_workspace_size(cu, k.shape[1], k.shape[2]), torch.uint8, q.device)
     else:
         _dev(ws, "ws", (ws.dtype,))
-    _check(lib().linear_chunk_attn(*head, _addr(cu), *tail, None if ws is None else ws.data_ptr(),
-                                   0 if ws is None else ws.numel() * ws.element_size(), _stream(stream)),
+    _check(lib().linear_chunk_attn(*head, addr, *tail, ws.data_ptr(), ws.numel() * ws.element_size(), s),
            "linear_chunk_attn")
     return out
 
