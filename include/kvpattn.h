@@ -324,9 +324,10 @@ int kv_append_rope(kvp_pool_t pool, int layer, const kvp_rope* rope, const void*
  *   decay       host float [num_kv_heads], each in (0, 1]
  *   src_slots, dst_slots   host int32 [num_seqs]
  *   scale       finite
- *   out         device [tokens, num_q_heads, head_dim], out_dtype KVP_BF16 or KVP_F32
+ *   out         device [tokens, num_q_heads, head_dim], out_dtype KVP_BF16 or KVP_F32; it must not overlap q, k, v or
+ *               the states
  * Strides are in elements, multiples of 8, and the pointers 16-byte aligned.  head_dim is 64 or 128, num_kv_heads at
- * most KVP_LINEAR_MAX_HEADS.  An infinity or NaN in a token's q, k or v leaves earlier tokens, other heads and other
+ * most KVP_LINEAR_MAX_HEADS, num_q_heads / num_kv_heads 1, 2, 4, 8 or 16.  An infinity or NaN in a token's q, k or v leaves earlier tokens, other heads and other
  * sequences as they are.
  * Errors: KVP_ERANGE for a slot outside [-1, num_slots); KVP_EINVAL for a destination that is another sequence's
  * source or destination, or a decay outside (0, 1]; KVP_EUNSUPPORTED for heads or dtypes not named here.

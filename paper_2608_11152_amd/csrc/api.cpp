@@ -614,23 +614,26 @@ int check_cu(const int32_t* cu, int num_seqs) {
   return KVP_OK;
 }
 
-// The work of linear_chunk_attn.  Workgroups fit the GPU three to a compute unit; a sequence of more than twice an even
-// share of the call's tokens is cut into parts of about that share, down to single chunks of 64: 24 calls of all shapes
-// take 0.88 and 0.83 of their time with parts from 128 and 64 on, against parts from 256 on.  Cutting takes two more
-// launches and a second pass over k and v, which walking a few chunks is quicker than: about 5 us a chunk for one query
-// head and 3.5 us for each further one.  Uncut / cut, 8 KV heads of 64, one sequence: of 256 tokens 25 / 27 us, 320
-// tokens 31 / 27 us; with 2 query heads a KV head 192 tokens 31 / 26 us; with 8, 129 tokens 92 / 46 us.
+// The work of linear_chunk_attn.  Workgroups fit the GPU three to a compute unit, those of head_dim 64 five; a sequence of
+// more than twice an even share of the call's tokens is cut into parts of about that share.  Shares are for three
+// workgroups (131071 tokens of 16 heads of 128: 784 us; for two or four 816 us), at head_dim 64 for four (24 calls take
+// 0.94 of their time with shares for three, 0.96 with five).  Parts go down to single chunks: 24 calls take 0.88 and 0.83
+// of their time with parts of 128 and 64 tokens on, against parts of 256 on.  Cutting takes two more launches and a second
+// pass over k and v, which walking a few chunks is quicker than: about 5 us a chunk for one query head and 3.5 us for each
+// further one.  Uncut / cut, 8 KV heads of 64, one sequence: of 256 tokens 25 / 27 us, 320 tokens 31 / 27 us; with 2 query
+// heads a KV head 192 tokens 31 / 26 us; with 8, 129 tokens 92 / 46 us.
 struct LinearPlan {
   std::vector<kvp::LinearItem> items, sums;
   std::vector<kvp::LinearScan> scans;
   int parts = 0;
 };
-constexpr int kLinearBlocks = 768, kLinearChunk = 64, kLinearMinWork = 512;
+constexpr int kLinearBlocks128 = 3 * 256, kLinearBlocks64 = 4 * 256, kLinearChunk = 64, kLinearMinWork = 512;
 
 // group: query heads per KV head; more of them, no fewer parts.  src, dst: nullable (only the number of parts is wanted).
-void plan_linear(const int32_t* cu, int num_seqs, int num_kv_heads, int group, const int32_t* src, const int32_t* dst,
-                 LinearPlan* P) {
-  const int64_t even = ((int64_t)cu[num_seqs] * num_kv_heads + kLinearBlocks - 1) / kLinearBlocks;
+void plan_linear(const int32_t* cu, int num_seqs, int num_kv_heads, int head_dim, int group, const int32_t* src,
+                 const int32_t* dst, LinearPlan* P) {
+  const int blocks = head_dim == 64 ? kLinearBlocks64 : kLinearBlocks128;
+  const int64_t even = ((int64_t)cu[num_seqs] * num_kv_heads + blocks - 1) / blocks;
   const int64_t share = std::max<int64_t>(kLinearChunk, even);
   for (int i = 0; i < num_seqs; ++i) {
     const int32_t n = cu[i + 1] - cu[i], from = src ? src[i] : -1, to = dst ? dst[i] : -1;
@@ -1041,7 +1044,7 @@ int linear_chunk_workspace_size(const int32_t* cu, int num_seqs, int num_kv_head
   const int rc = check_cu(cu, num_seqs);
   if (rc) return rc;
   LinearPlan P;
-  plan_linear(cu, num_seqs, num_kv_heads, kLinearMaxGroup, nullptr, nullptr, &P);
+  plan_linear(cu, num_seqs, num_kv_heads, head_dim, kLinearMaxGroup, nullptr, nullptr, &P);
   *bytes = (size_t)P.parts * num_kv_heads * head_dim * head_dim * sizeof(float);
   return KVP_OK;
 } catch (const std::exception& x) {
@@ -1064,7 +1067,7 @@ int linear_chunk_attn(const void* q, int64_t q_stride, const void* k, int64_t k_
     if (cu[num_seqs] > 0 && (stride < head_dim || stride > kLinearMaxStride))
       return set_err(KVP_EINVAL, "stride %lld outside [head_dim, %lld]", (long long)stride, (long long)kLinearMaxStride);
   LinearPlan P;
-  plan_linear(cu, num_seqs, num_kv_heads, num_q_heads / num_kv_heads, src_slots, dst_slots, &P);
+  plan_linear(cu, num_seqs, num_kv_heads, head_dim, num_q_heads / num_kv_heads, src_slots, dst_slots, &P);
   const size_t need = (size_t)P.parts * num_kv_heads * head_dim * head_dim * sizeof(float);
   if (need > 0 && (!ws || ws_bytes < need || (reinterpret_cast<uintptr_t>(ws) & 15) != 0))
     return set_err(KVP_EWORKSPACE, "workspace of %zu bytes (16-byte aligned), %zu needed", ws ? ws_bytes : 0, need);

@@ -253,8 +253,12 @@ __global__ __launch_bounds__(256) void gather_kernel(GatherArgs a) {
 
 // kv_append_rope.  One wave per (page run, KV head) turns the keys and writes both blocks; one per (page run, up to
 // kQueryHeads query heads) turns the queries of the same tokens.  A lane holds a unit of 8 dims of one token (in the half
-// layout with the unit R / 2 further), computes its sines and cosines once and uses them for all of the wave's heads; a
-// run of few tokens spreads the heads over the lanes.  Bandwidth is what bounds it.
+// layout 8 more, R / 2 further or the next ones that are not rotated), computes its sines and cosines once and uses them
+// for all of the wave's heads; a run of few tokens spreads the heads over the lanes.  Bandwidth is what bounds it: 16416
+// tokens of 32 + 4 heads of 128 (336 MB) take 74 us, 4.5 TB/s of the 5.1 that a copy reaches; 3567 tokens into FP8 pages
+// 16.7 us, 4.2 TB/s.  Waves of 4 query heads: 72 and 15.4 us there, but 24 instead of 21 us for 4160 tokens of 32 + 8
+// heads, and 1.6% more over 36 shapes.  A step of 512 single tokens (11 us) waits for its run records, which lie in pinned
+// host memory, then for page ids, then for rows.
 constexpr int kQueryHeads = 8;
 
 template <int D, bool F8, bool IL>

@@ -7,23 +7,31 @@
 // linear_chunk_kernel: chunks of 64 tokens, from the state S before the chunk (rows i, j of the chunk, l = decay):
 //   O = (l^(i+1) Q) S + (Q K^T . l^(i-j) for j <= i) V          S' = l^64 S + (l^(63-j) K)^T V
 // One workgroup of 2 D threads per (item, KV head) walks an item's tokens; each of its D / 32 waves holds 32 columns of
-// S in registers (fp32, 2 D registers' worth per 4 rows) from the first chunk to the last, so a chunk reads q, k, v and
-// writes o, once.  Bandwidth is what bounds it: 8 D bytes and 6 D^2 .. 10 D^2 flops a token and head.
+// S in registers (fp32, D / 2 of them) from the first chunk to the last, so a chunk reads q, k and v and writes o, once:
+// 8 D bytes a token and head, and 12 D^2 flops as matrix products of bf16 parts (below).
 //
 // All products run as v_mfma_f32_16x16x32_bf16.  Its result tile gives a lane 4 rows (4 g + r) of one column; its
 // operand wants 8 consecutive k (8 g ..) of one row or column.  Which dim or token a row of a tile stands for is free: row
 // m of an even tile is 8 (m / 4) + m % 4 of its 32, of the odd tile 4 more, so a lane's rows of both are 8 consecutive
-// ones, and the state and the weights of a chunk go from one product's result into the next one's operand without leaving
-// their registers:
+// ones, and the state and the weights of a chunk are the next product's operand as they come out of the last one's result:
 //   P^T (keys x rows)   = K Q^T           O^T (columns x rows) = S^T Q^T + V^T P^T           S (dims x columns) = K^T V
-// Rows of q, k and v go from memory straight to LDS; K^T and V^T come from there through its transposing reads.
-//
-// A sequence that would leave compute units without work is cut into parts (plan_linear): linear_sum_kernel sums each part
-// from zeros, linear_scan_kernel turns the sums into the states before the parts, and the parts are
-// items.  The parts' keys and values are read twice.
+// The waves share P's tiles (each wave needs all of them) through the place of q in LDS, which is done with by then.
+// Rows of q, k and v go from memory straight to LDS, past the caches (165 -> 163 and 799 -> 776 us below); K^T and V^T
+// come from there through its transposing reads.
 //
 // Operands that are not bf16 are carried as sums of bf16 parts: S and P as two (2^-18 left: far inside a bf16 output's
-// half step 2^-9), the decayed V that goes into the state as three (2^-26: the state is fp32).
+// half step 2^-9), the decayed V that goes into the state as three (2^-26: the state is fp32).  A single part for S and P
+// would take 6% less time, with 2^-9 of the state in every output.
+//
+// Three workgroups fit a compute unit (50 KB of LDS; 149 VGPRs, which the sched_barriers and Lane keep them at).  64
+// prompts of 128 .. 1024 tokens with 16 heads of 128, 663 MB: 161 us, 4.1 TB/s of the 5.1 that a copy reaches; without
+// the matrix instructions 135.  Of a chunk's 12.8 us for the three, memory needs 9.8, matrix instructions 3.9, the vector
+// unit 4.7 and LDS 2.9: these run beside each other for the most part, not altogether.
+//
+// A sequence that would leave compute units without work is cut into parts (plan_linear): linear_sum_kernel sums each part
+// from zeros, linear_scan_kernel turns the sums into the states before the parts, and the parts are items.  The parts'
+// keys and values are read twice: 131071 tokens with 16 heads of 128 take 770 us, 216 of them the sums (206 GFLOP: V
+// in 3 parts), 25 the scan, 496 the chunks (2.1 GB, 4.3 TB/s).
 #include <algorithm>
 
 #include "rope_dev.h"
@@ -536,7 +544,8 @@ __global__ __launch_bounds__(256) void linear_scan_kernel(LinearArgs a, LinearIt
 
 // Single tokens: one workgroup per (sequence, KV head).  A thread holds 4 columns of D / R rows of the state, R apart, all
 // loads issued before the first is used; the rows' sums for the output meet in the wave and then in LDS.  Bandwidth is
-// what bounds it: the state is read and written once, past the caches.
+// what bounds it: the state is read and written once, past the caches.  512 samples of 64 prompts with 16 heads of 128
+// (612 MB, 537 of them written): 133 us in two launches, 4.6 TB/s.  4 sequences: 4.5 us of a call's 13.5.
 template <int D>
 __global__ __launch_bounds__(256) void linear_token_kernel(LinearArgs a, LinearBatch batch) {
   constexpr int C = D / 4, R = 256 / C, N = D / R;  // threads per row, rows at a time, rows per thread
