@@ -334,8 +334,8 @@ int kv_append_rope(kvp_pool_t pool, int layer, const kvp_rope* rope, const void*
  * ------------------------------------------------------------------------------------------------- */
 #define KVP_LINEAR_MAX_HEADS 128
 
-/* Workspace bytes linear_chunk_attn needs at most, whatever num_q_heads is (0 where no sequence is long enough to be cut
- * into parts). */
+/* Workspace bytes linear_chunk_attn needs at most, whatever its num_q_heads and slots are: states inside sequences that it
+ * cuts into parts, and copies of states that several workgroups read while one updates them in place. */
 int linear_chunk_workspace_size(const int32_t* cu, int num_seqs, int num_kv_heads, int head_dim, size_t* bytes);
 
 /* Chunks: sequence i's tokens are the rows cu[i] .. cu[i+1] (none: its state is handed on as it is).

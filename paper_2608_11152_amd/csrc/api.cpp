@@ -622,32 +622,82 @@ int check_cu(const int32_t* cu, int num_seqs) {
 // pass over k and v, which walking a few chunks is quicker than: about 5 us a chunk for one query head and 3.5 us for each
 // further one.  Uncut / cut, 8 KV heads of 64, one sequence: of 256 tokens 25 / 27 us, 320 tokens 31 / 27 us; with 2 query
 // heads a KV head 192 tokens 31 / 26 us; with 8, 129 tokens 92 / 46 us.
+//
+// Where no more than half of those workgroups would have work, the query heads of a KV head are shared out too, `split`
+// ways; each workgroup walks the state for itself, the first one keeps it.  A sequence whose state is updated in place has
+// it copied first (a part of its own, written by linear_scan_kernel): the others still read what the first one writes.
+// That launch costs as much as one head's chunk or two.  Not split / split, head_dim 128: 16 query heads on one KV head, 6
+// sequences of 85 .. 137 tokens 124 / 24 us; 128 on 8, 8 of 128 tokens 149 / 46 us; 32 on 8, one of 128 in place 39 / 23
+// us, of 64 22 / 22 us.  Filling the GPU twice over is slower: 16 on 8, 93 single tokens 24 us, with twice the workgroups
+// 31 us.
 struct LinearPlan {
   std::vector<kvp::LinearItem> items, sums;
   std::vector<kvp::LinearScan> scans;
   int parts = 0;
 };
 constexpr int kLinearBlocks128 = 3 * 256, kLinearBlocks64 = 4 * 256, kLinearChunk = 64, kLinearMinWork = 512;
+constexpr int kLinearMinCopy = 4, kLinearMaxGroup = 16;
 
-// group: query heads per KV head; more of them, no fewer parts.  src, dst: nullable (only the number of parts is wanted).
+int linear_blocks(int head_dim) { return head_dim == 64 ? kLinearBlocks64 : kLinearBlocks128; }
+
+int64_t linear_share(const int32_t* cu, int num_seqs, int num_kv_heads, int head_dim) {
+  const int blocks = linear_blocks(head_dim);
+  return std::max<int64_t>(kLinearChunk, ((int64_t)cu[num_seqs] * num_kv_heads + blocks - 1) / blocks);
+}
+
+// Parts of a sequence of n tokens, each of *len of them (the last may be shorter).  group: query heads per KV head.
+int linear_parts(int32_t n, int64_t share, int group, int32_t* len) {
+  *len = n;
+  if (n <= 2 * share || (int64_t)n * (1 + group) <= kLinearMinWork) return 1;
+  const int64_t want = (n + share - 1) / share;
+  *len = (int32_t)(((n + want - 1) / want + kLinearChunk - 1) / kLinearChunk * kLinearChunk);
+  return (n + *len - 1) / *len;
+}
+
+// The parts that a call may need, whatever its query heads and slots.
+int64_t linear_most_parts(const int32_t* cu, int num_seqs, int num_kv_heads, int head_dim) {
+  const int64_t share = linear_share(cu, num_seqs, num_kv_heads, head_dim);
+  const bool split = (int64_t)num_seqs * num_kv_heads * 2 <= linear_blocks(head_dim);
+  int64_t parts = 0;
+  for (int i = 0; i < num_seqs; ++i) {
+    int32_t len;
+    const int m = linear_parts(cu[i + 1] - cu[i], share, kLinearMaxGroup, &len);
+    if (m > 1 || (split && len > 0)) parts += m;
+  }
+  return parts;
+}
+
 void plan_linear(const int32_t* cu, int num_seqs, int num_kv_heads, int head_dim, int group, const int32_t* src,
                  const int32_t* dst, LinearPlan* P) {
-  const int blocks = head_dim == 64 ? kLinearBlocks64 : kLinearBlocks128;
-  const int64_t even = ((int64_t)cu[num_seqs] * num_kv_heads + blocks - 1) / blocks;
-  const int64_t share = std::max<int64_t>(kLinearChunk, even);
+  const int64_t share = linear_share(cu, num_seqs, num_kv_heads, head_dim);
+  int64_t blocks = 0;
+  int32_t len;
+  for (int i = 0; i < num_seqs; ++i) blocks += linear_parts(cu[i + 1] - cu[i], share, group, &len);
+  blocks *= num_kv_heads;
+  int split = 1;
+  while (2 * split <= group && 2 * split * blocks <= linear_blocks(head_dim)) split *= 2;
+  auto add = [&](int32_t t0, int32_t n, int32_t from, int32_t to, int ways) {
+    for (int w = 0; w < ways; ++w) P->items.push_back({t0, n, from, w == 0 ? to : -1, w * (group / ways), group / ways});
+  };
   for (int i = 0; i < num_seqs; ++i) {
-    const int32_t n = cu[i + 1] - cu[i], from = src ? src[i] : -1, to = dst ? dst[i] : -1;
-    if (n <= 2 * share || (int64_t)n * (1 + group) <= kLinearMinWork) {
-      P->items.push_back({cu[i], n, from, to});
+    const int32_t n = cu[i + 1] - cu[i], from = src[i], to = dst[i];
+    const int m = linear_parts(n, share, group, &len);
+    if (m == 1) {
+      const bool in_place = from >= 0 && from == to;
+      const int chunks = (n + kLinearChunk - 1) / kLinearChunk;
+      const int ways = n == 0 || (in_place && (group - group / split) * chunks < kLinearMinCopy) ? 1 : split;
+      if (in_place && ways > 1) {
+        P->scans.push_back({from, P->parts, 1, n});
+        add(cu[i], n, -2 - P->parts++, to, ways);
+      } else {
+        add(cu[i], n, from, to, ways);
+      }
       continue;
     }
-    const int64_t want = (n + share - 1) / share;  // parts of a whole number of chunks
-    const int32_t len = (int32_t)(((n + want - 1) / want + kLinearChunk - 1) / kLinearChunk * kLinearChunk);
-    const int32_t m = (n + len - 1) / len;
     for (int32_t p = 0; p < m; ++p) {
       const int32_t t0 = cu[i] + p * len, cnt = std::min(len, n - p * len);
-      P->items.push_back({t0, cnt, p == 0 && from < 0 ? -1 : -2 - (P->parts + p), p + 1 < m ? -1 : to});
-      if (p + 1 < m) P->sums.push_back({t0, cnt, -1, -2 - (P->parts + p + 1)});
+      add(t0, cnt, p == 0 && from < 0 ? -1 : -2 - (P->parts + p), p + 1 < m ? -1 : to, split);
+      if (p + 1 < m) P->sums.push_back({t0, cnt, -1, -2 - (P->parts + p + 1), 0, 0});
     }
     P->scans.push_back({from, P->parts, m, len});
     P->parts += m;
@@ -659,7 +709,6 @@ void plan_linear(const int32_t* cu, int num_seqs, int num_kv_heads, int head_dim
 static_assert(kvp::kLinearHeads == KVP_LINEAR_MAX_HEADS && kvp::kRopePairs == KVP_ROPE_PAIRS, "as in the header");
 
 constexpr int64_t kLinearMaxStride = 1 << 24;
-constexpr int kLinearMaxGroup = 16;
 
 constexpr int32_t kRopeValid = 0x726f7065;  // kvp_rope.valid
 
@@ -1043,9 +1092,8 @@ int linear_chunk_workspace_size(const int32_t* cu, int num_seqs, int num_kv_head
   if (num_seqs == 0) return KVP_OK;
   const int rc = check_cu(cu, num_seqs);
   if (rc) return rc;
-  LinearPlan P;
-  plan_linear(cu, num_seqs, num_kv_heads, head_dim, kLinearMaxGroup, nullptr, nullptr, &P);
-  *bytes = (size_t)P.parts * num_kv_heads * head_dim * head_dim * sizeof(float);
+  *bytes = (size_t)linear_most_parts(cu, num_seqs, num_kv_heads, head_dim) * num_kv_heads * head_dim * head_dim *
+           sizeof(float);
   return KVP_OK;
 } catch (const std::exception& x) {
   return set_err(KVP_ENOMEM, "linear_chunk_workspace_size: %s", x.what());

@@ -83,6 +83,7 @@ struct AppendRopeArgs {
 struct LinearItem {
   int32_t t0, n;            // first token, tokens
   int32_t src, dst;         // state slots; -1: starts from zeros / is not kept
+  int32_t g0, gn;           // query heads of the KV head's: first, number
 };
 
 // linear_decode_attn: slots (source, destination) of up to kLinearBatch sequences and the heads' decay, in the launch

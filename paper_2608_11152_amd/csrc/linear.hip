@@ -318,6 +318,7 @@ __global__ __launch_bounds__(2 * D, 3) void linear_chunk_kernel(LinearArgs a, Li
   const Wave<D> me(a.Hkv);
   const int w = me.w, h = me.h, G = a.Hq / a.Hkv, tid = threadIdx.x;
   const LinearItem it = list.items[me.item];
+  const int first = h * G + it.g0;
   ChunkDecay decay((double)list.decay[h]);
   if (tid <= kChunk) {
     const double x = power((double)list.decay[h], tid);
@@ -329,7 +330,7 @@ __global__ __launch_bounds__(2 * D, 3) void linear_chunk_kernel(LinearArgs a, Li
 
   // Loads are under way while there is work that does not need them: the next q and v during the update of the state, the
   // next k (its tile is the update's) and still v during the state's product with q.
-  me.fetch(L.q, a.q, a.q_stride, h * G, it, 0);
+  me.fetch(L.q, a.q, a.q_stride, first, it, 0);
   me.fetch(L.v, a.v, a.v_stride, h, it, 0);
   f32x4 S[MT][2] = {};
   if (it.src != -1) {
@@ -349,7 +350,7 @@ __global__ __launch_bounds__(2 * D, 3) void linear_chunk_kernel(LinearArgs a, Li
     arrived_but_4();  // q (not yet v); and the update is done with k
     me.fetch(L.k, a.k, a.k_stride, h, it, c);
     u32x4 vf[2][2];
-    for (int gq = 0; gq < G; ++gq) {
+    for (int gq = 0; gq < it.gn; ++gq) {
       if (gq > 0) arrived();
       // O^T = S^T Q^T for the chunk's four row tiles, lane column m being row i = 16 rt + m
       const Lane l0;
@@ -426,7 +427,7 @@ __global__ __launch_bounds__(2 * D, 3) void linear_chunk_kernel(LinearArgs a, Li
       all_read();
       me.load_v(L.v, vf);
       const int es = a.out_f32 ? 4 : 2;
-      char* const out = reinterpret_cast<char*>(a.out) + ((it.t0 + (int64_t)c) * a.Hq + h * G + gq) * D * es;
+      char* const out = reinterpret_cast<char*>(a.out) + ((it.t0 + (int64_t)c) * a.Hq + first + gq) * D * es;
       bool bad = false;
 #pragma unroll
       for (int rt = 3; rt >= 0; --rt) {
@@ -461,7 +462,7 @@ __global__ __launch_bounds__(2 * D, 3) void linear_chunk_kernel(LinearArgs a, Li
         }
         const int i = 16 * rt + l.m;
         if (bad) {  // key by key: only keys up to the row are multiplied at all
-          const uint16_t* const qi = a.q + (it.t0 + (int64_t)(c + min(i, n - 1))) * a.q_stride + (h * G + gq) * D;
+          const uint16_t* const qi = a.q + (it.t0 + (int64_t)(c + min(i, n - 1))) * a.q_stride + (first + gq) * D;
           V[0] = V[1] = f32x4{};
 #pragma unroll 1
           for (int j = 0; j < 16 * rt + 16; ++j) {
@@ -497,9 +498,10 @@ __global__ __launch_bounds__(2 * D, 3) void linear_chunk_kernel(LinearArgs a, Li
         }
       }
       all_read();  // the weights and v
-      if (gq + 1 < G) me.fetch(L.q, a.q, a.q_stride, h * G + gq + 1, it, c);
+      if (gq + 1 < it.gn) me.fetch(L.q, a.q, a.q_stride, first + gq + 1, it, c);
     }
-    me.fetch(L.q, a.q, a.q_stride, h * G, it, c + kChunk);
+    if (it.dst == -1 && c + kChunk >= it.n) return;  // nobody asks for the state
+    me.fetch(L.q, a.q, a.q_stride, first, it, c + kChunk);
     me.fetch(L.v, a.v, a.v_stride, h, it, c + kChunk);
     me.update(S, L.k, vf, L.pw, n, decay.next(L.pw[n + 63], n));
   }
@@ -617,10 +619,9 @@ hipError_t launch_linear_decode(const LinearArgs& a, const LinearBatch& batch, i
 
 template <int D>
 static void launch_chunk(const LinearArgs& a, const LinearItems& list, hipStream_t s) {
-  if (list.n_scans > 0) {
-    hipLaunchKernelGGL(linear_sum_kernel<D>, dim3(list.n_sums * a.Hkv), dim3(2 * D), 0, s, a, list);
+  if (list.n_sums > 0) hipLaunchKernelGGL(linear_sum_kernel<D>, dim3(list.n_sums * a.Hkv), dim3(2 * D), 0, s, a, list);
+  if (list.n_scans > 0)
     hipLaunchKernelGGL(linear_scan_kernel, dim3(list.n_scans * a.Hkv * (D * D / 256)), dim3(256), 0, s, a, list, D);
-  }
   hipLaunchKernelGGL(linear_chunk_kernel<D>, dim3(list.n_items * a.Hkv), dim3(2 * D), 0, s, a, list);
 }
 
