@@ -1141,6 +1141,7 @@ int linear_chunk_attn(const void* q, int64_t q_stride, const void* k, int64_t k_
   list.n_items = (int)P.items.size();
   list.n_sums = (int)P.sums.size();
   list.n_scans = (int)P.scans.size();
+  for (const kvp::LinearScan& scan : P.scans) list.most_parts = std::max(list.most_parts, scan.n);
   const hipError_t e = kvp::launch_linear_chunk(a, list, head_dim, s);
   const int rr = staging().release(lease, e == hipSuccess);
   return e == hipSuccess ? rr : hip_err(e, "linear_chunk_attn launch");

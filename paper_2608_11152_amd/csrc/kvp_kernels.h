@@ -107,6 +107,7 @@ struct LinearItems {
   const LinearScan* scans;
   const float* decay;
   int n_items, n_sums, n_scans;
+  int most_parts;           // of a scan
 };
 
 struct LinearArgs {

@@ -31,7 +31,7 @@
 // A sequence that would leave compute units without work is cut into parts (plan_linear): linear_sum_kernel sums each part
 // from zeros, linear_scan_kernel turns the sums into the states before the parts, and the parts are items.  The parts'
 // keys and values are read twice: 131071 tokens with 16 heads of 128 take 770 us, 216 of them the sums (206 GFLOP: V
-// in 3 parts), 25 the scan, 496 the chunks (2.1 GB, 4.3 TB/s).
+// in 3 parts), 19 the scan, 496 the chunks (2.1 GB, 4.3 TB/s).
 #include <algorithm>
 
 #include "rope_dev.h"
@@ -516,32 +516,66 @@ __global__ __launch_bounds__(2 * D, 3) void linear_chunk_kernel(LinearArgs a, Li
 }
 
 // States before each part of the long sequences, from the parts' own sums: S_0 = source, S_i = l^len S_(i-1) + sum_(i-1).
-// Slot i of a sequence's parts holds sum_(i-1) before and S_i afterwards.  One thread per element, in 64 bits: the decay
-// of one part meets that of hundreds.
+// Slot i of a sequence's parts holds sum_(i-1) before and S_i afterwards.  In 64 bits: the decay of one part meets that of
+// hundreds.  A thread takes 4 elements; `Ways` of them share out the parts of an element, meet, and go on from the sum of
+// those before.  The chain of loads is what bounds it, or where there are few parts, the powers of the decay that each
+// thread takes: up to Ways * U parts every load is issued before the first is used, and kept; beyond that the parts are
+// read twice, U at a time.  1 head of 64, 25000 tokens in 390 parts, with 2 / 4 / 16 ways (U = 8, 16, 8): 65 / 36 / 16 us
+// (a thread an element: 103); 16 heads of 128, 131071 tokens in 47: 27 / 19 / 28 us; 9 sequences of 3500 tokens in 5 parts
+// each: 22 / 39 / 106 us.
+template <int Ways, int U>
 __global__ __launch_bounds__(256) void linear_scan_kernel(LinearArgs a, LinearItems list, int D) {
-  const int per = D * D / 256, e = (blockIdx.x % per) * 256 + threadIdx.x;
+  constexpr int kScanLanes = 256 / Ways, kScanElements = 4 * kScanLanes;
+  __shared__ double sums[Ways][kScanElements];
+  const int lane = threadIdx.x % kScanLanes, way = threadIdx.x / kScanLanes;
+  const int per = D * D / kScanElements, e = (blockIdx.x % per) * kScanElements + 4 * lane;
   const int h = blockIdx.x / per % a.Hkv;
   const LinearScan sc = list.scans[blockIdx.x / per / a.Hkv];
+  f32x4* const p = reinterpret_cast<f32x4*>(state_at(a, -2 - sc.part, h, D) + e);
+  const int64_t step = (int64_t)a.Hkv * D * D / 4;
+  f32x4 source{};
+  if (sc.src >= 0) source = *reinterpret_cast<const f32x4*>(state_at(a, sc.src, h, D) + e);
+  const int m = (sc.n - 1 + Ways - 1) / Ways, lo = 1 + way * m, hi = min(lo + m, sc.n);
+  f32x4 x[U];
+  auto load = [&](int i) {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (i + u < hi) x[u] = p[(i + u) * step];
+  };
+  if (m <= U) load(lo);
   const double f = power((double)list.decay[h], sc.len);
-  float* p = state_at(a, -2 - sc.part, h, D) + e;
-  const int64_t step = (int64_t)a.Hkv * D * D;
-  double S = 0.0;
-  if (sc.src >= 0) {
-    const float x = state_at(a, sc.src, h, D)[e];
-    p[0] = x;
-    S = x;
-  }
-  constexpr int U = 16;  // loads in flight
-  for (int i = 1; i < sc.n; i += U) {
-    float x[U];
+  double S[4] = {};
+  for (int i = lo; i < hi; i += U) {
+    if (m > U) load(i);
 #pragma unroll
-    for (int u = 0; u < U; ++u) x[u] = i + u < sc.n ? p[(i + u) * step] : 0.0f;
+    for (int u = 0; u < U; ++u)
+      if (i + u < hi)
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      S = fma(S, f, (double)x[u]);
-      if (i + u < sc.n) p[(i + u) * step] = (float)S;
-    }
+        for (int b = 0; b < 4; ++b) S[b] = fma(S[b], f, (double)x[u][b]);
   }
+#pragma unroll
+  for (int b = 0; b < 4; ++b) sums[way][4 * lane + b] = S[b];
+  __syncthreads();
+  const double over = power(f, m);
+#pragma unroll
+  for (int b = 0; b < 4; ++b) S[b] = source[b];
+  for (int w = 0; w < way; ++w)
+#pragma unroll
+    for (int b = 0; b < 4; ++b) S[b] = fma(S[b], over, sums[w][4 * lane + b]);
+  for (int i = lo; i < hi; i += U) {
+    if (m > U) load(i);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (i + u < hi) {
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+          S[b] = fma(S[b], f, (double)x[u][b]);
+          x[u][b] = (float)S[b];
+        }
+        p[(i + u) * step] = x[u];
+      }
+  }
+  if (way == 0 && sc.src >= 0) p[0] = source;
 }
 
 // Single tokens: one workgroup per (sequence, KV head).  A thread holds 4 columns of D / R rows of the state, R apart, all
@@ -617,11 +651,18 @@ hipError_t launch_linear_decode(const LinearArgs& a, const LinearBatch& batch, i
   return hipGetLastError();
 }
 
+template <int Ways, int U>
+static void launch_scan(const LinearArgs& a, const LinearItems& list, int D, hipStream_t s) {
+  const dim3 grid(list.n_scans * a.Hkv * (D * D * Ways / 1024));
+  hipLaunchKernelGGL((linear_scan_kernel<Ways, U>), grid, dim3(256), 0, s, a, list, D);
+}
+
 template <int D>
 static void launch_chunk(const LinearArgs& a, const LinearItems& list, hipStream_t s) {
   if (list.n_sums > 0) hipLaunchKernelGGL(linear_sum_kernel<D>, dim3(list.n_sums * a.Hkv), dim3(2 * D), 0, s, a, list);
-  if (list.n_scans > 0)
-    hipLaunchKernelGGL(linear_scan_kernel, dim3(list.n_scans * a.Hkv * (D * D / 256)), dim3(256), 0, s, a, list, D);
+  if (list.most_parts > 64) launch_scan<16, 8>(a, list, D, s);
+  else if (list.most_parts > 32) launch_scan<4, 16>(a, list, D, s);
+  else if (list.most_parts > 0) launch_scan<2, 8>(a, list, D, s);
   hipLaunchKernelGGL(linear_chunk_kernel<D>, dim3(list.n_items * a.Hkv), dim3(2 * D), 0, s, a, list);
 }
 

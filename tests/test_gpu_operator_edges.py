@@ -151,3 +151,17 @@ def test_two_streams_at_once():
     torch.cuda.synchronize()
     for (outs, state), c, g in zip(alone, cases, got):
         assert all(torch.equal(a, b) for a, b in zip(outs, g)) and torch.equal(state, c.state)
+
+
+@pytest.mark.parametrize("lens", [[1000], [2048, 70], [2049], [2600, 2200], [4160]])
+@pytest.mark.parametrize("Hq,Hkv,d,src", [(1, 1, 64, 0), (4, 2, 128, 0), (2, 1, 64, -1)])
+def test_linear_numbers_of_parts(lens, Hq, Hkv, d, src):
+    """16 to 65 parts of 64 tokens: every way that the states between them are summed."""
+    import torch
+    note(f"linear parts {lens} {Hq}/{Hkv} {d} {src}")
+    c = Case(lens, Hq, Hkv, d, decay=[0.9997, 1.0][:Hkv])
+    slots = list(range(len(lens)))
+    want, room = c.oracle(slots if src == 0 else [-1] * len(lens), slots, d ** -0.5)
+    out = kp.linear_chunk_attn(c.q, c.k, c.v, c.state, c.decay, slots if src == 0 else [-1] * len(lens), slots, c.cu,
+                               out_dtype=torch.float32)
+    check(out, c.state, want, room, c, slots)
