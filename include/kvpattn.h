@@ -285,7 +285,7 @@ int kvp_rope_init(kvp_rope* rope, int rotary_dim, int interleaved, double base, 
  *              t * token_stride + h * head_stride.  y may be x with the same strides, or must not overlap it; y's
  *              heads must not overlap each other.
  *   positions  device int32 [num_tokens], any values
- *   head_dim   rotary_dim..256
+ *   num_heads  at most 2^20;  head_dim  rotary_dim..256
  * Computed in fp32 (the angle modulo a turn in 64-bit integers) and rounded once.  Reads no host memory after it
  * returns, so it can be captured. */
 int kvp_rope_apply(const kvp_rope* rope, const void* x, int64_t x_token_stride, int64_t x_head_stride, void* y,
@@ -300,8 +300,8 @@ int kvp_rope_apply(const kvp_rope* rope, const void* x, int64_t x_token_stride, 
  *   q       device bf16, nullable (then q_out and num_q_heads are ignored): token t's num_q_heads * head_dim elements
  *           from t * q_stride.  q_out likewise; it may be q with the same stride, or must not overlap it.
  * Strides are in elements, multiples of 8, and the pointers 16-byte aligned; q_out_stride is at least
- * num_q_heads * head_dim.  rotary_dim is at most head_dim.  The pool must live on the current device.  Everything else
- * as in kv_append; a token whose page id is outside the pool is skipped, its query is turned all the same. */
+ * num_q_heads * head_dim, num_q_heads a multiple of num_kv_heads and at most 2^20.  rotary_dim is at most head_dim.  The
+ * pool must live on the current device.  Everything else as in kv_append; a token whose page id is outside the pool is skipped, its query is turned all the same. */
 int kv_append_rope(kvp_pool_t pool, int layer, const kvp_rope* rope, const void* k, int64_t k_stride, const void* v,
                    int64_t v_stride, const void* q, int64_t q_stride, void* q_out, int64_t q_out_stride,
                    int num_q_heads, const int32_t* block_tables, int maxp, const int32_t* start_pos,

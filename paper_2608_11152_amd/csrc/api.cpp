@@ -711,6 +711,7 @@ static_assert(kvp::kLinearHeads == KVP_LINEAR_MAX_HEADS && kvp::kRopePairs == KV
 constexpr int64_t kLinearMaxStride = 1 << 24;
 
 constexpr int32_t kRopeValid = 0x726f7065;  // kvp_rope.valid
+constexpr int kRopeMaxHeads = 1 << 20;      // the kernels' thread indices have 31 bits for a token's heads and dims
 
 // Rows of bf16 that a kernel reads or writes 16 bytes at a time.
 int check_rows(const void* p, int64_t stride, const char* name) {
@@ -976,6 +977,8 @@ int kv_append_rope(kvp_pool_t pool, int layer, const kvp_rope* rope, const void*
     if (!rc && (num_q_heads <= 0 || num_q_heads % pool->num_kv_heads))
       rc = set_err(KVP_EUNSUPPORTED, "num_q_heads %d is not a multiple of the pool's %d KV heads", num_q_heads,
                    pool->num_kv_heads);
+    if (!rc && num_q_heads > kRopeMaxHeads)
+      rc = set_err(KVP_EUNSUPPORTED, "num_q_heads %d above %d", num_q_heads, kRopeMaxHeads);
     if (!rc && q_out_stride < (int64_t)num_q_heads * pool->head_dim)
       rc = set_err(KVP_EINVAL, "q_out stride %lld is less than a row of %d heads", (long long)q_out_stride, num_q_heads);
     if (!rc && q_out == q && q_out_stride != q_stride)
@@ -1051,6 +1054,7 @@ int kvp_rope_apply(const kvp_rope* rope, const void* x, int64_t x_token_stride, 
   if (dtype != KVP_BF16 && dtype != KVP_F32) return set_err(KVP_EUNSUPPORTED, "dtype %d (KVP_BF16 or KVP_F32)", dtype);
   if (num_tokens < 0 || num_heads < 0)
     return set_err(KVP_EINVAL, "num_tokens %lld or num_heads %d negative", (long long)num_tokens, num_heads);
+  if (num_heads > kRopeMaxHeads) return set_err(KVP_EUNSUPPORTED, "num_heads %d above %d", num_heads, kRopeMaxHeads);
   if (num_tokens == 0 || num_heads == 0) return KVP_OK;
   if (!x || !y || !positions) return set_err(KVP_EINVAL, "x, y or positions is NULL");
   const uintptr_t es = dtype == KVP_F32 ? 4 : 2;
@@ -1061,9 +1065,14 @@ int kvp_rope_apply(const kvp_rope* rope, const void* x, int64_t x_token_stride, 
   if (x_token_stride < 0 || x_head_stride < 0) return set_err(KVP_EINVAL, "negative x stride");
   // y's heads are apart: inside a token, and from token to token (or the other way round)
   const int64_t ts = y_token_stride, hs = y_head_stride;
-  const bool inner_heads = (num_heads == 1 || hs >= head_dim) && (num_tokens == 1 || ts >= (num_heads - 1) * hs + head_dim);
-  const bool inner_tokens = (num_tokens == 1 || ts >= head_dim) && (num_heads == 1 || hs >= (num_tokens - 1) * ts + head_dim);
+  const __int128 heads_end = (__int128)(num_heads - 1) * hs + head_dim, tokens_end = (__int128)(num_tokens - 1) * ts + head_dim;
+  const bool inner_heads = (num_heads == 1 || hs >= head_dim) && (num_tokens == 1 || ts >= heads_end);
+  const bool inner_tokens = (num_tokens == 1 || ts >= head_dim) && (num_heads == 1 || hs >= tokens_end);
   if (ts < 0 || hs < 0 || !(inner_heads || inner_tokens)) return set_err(KVP_EINVAL, "y's heads overlap");
+  const auto far = [&](int64_t token, int64_t head) {
+    return (__int128)(num_tokens - 1) * token + (__int128)(num_heads - 1) * head > INT64_MAX / 8;
+  };
+  if (far(x_token_stride, x_head_stride) || far(ts, hs)) return set_err(KVP_EINVAL, "strides beyond 64 bits of bytes");
   if (x == y && ((num_tokens > 1 && x_token_stride != ts) || (num_heads > 1 && x_head_stride != hs)))
     return set_err(KVP_EINVAL, "y is x with other strides");
   kvp::RopeArgs a{};

@@ -165,3 +165,20 @@ def test_linear_numbers_of_parts(lens, Hq, Hkv, d, src):
     out = kp.linear_chunk_attn(c.q, c.k, c.v, c.state, c.decay, slots if src == 0 else [-1] * len(lens), slots, c.cu,
                                out_dtype=torch.float32)
     check(out, c.state, want, room, c, slots)
+
+
+def test_append_rope_refuses_more_heads_than_its_indices_hold():
+    import torch
+    note("append rope heads")
+    Hq, Hkv, d = (1 << 20) + 16, 16, 64
+    q = torch.zeros(1, Hq, d, dtype=torch.bfloat16, device="cuda")
+    k = torch.ones(1, Hkv, d, dtype=torch.bfloat16, device="cuda")
+    pool = kp.Pool(1, 2, Hkv, d)
+    bt = torch.tensor([[1]], dtype=torch.int32, device="cuda")
+    with pytest.raises(kp.KvpError) as e:
+        kp.kv_append_rope(pool, 0, kp.Rope(64), k, k, bt, [0], [0, 1], q=q)
+    assert e.value.code == kp.KVP_EUNSUPPORTED and not bool(pool.layer_raw().any())
+    got = kp.kv_append_rope(pool, 0, kp.Rope(64), k, k, bt, [3], [0, 1], q=torch.ones_like(q[:, :1 << 20]))
+    one = kp.kvp_rope_apply(kp.Rope(64), torch.ones_like(q[:, :1]), torch.tensor([3], dtype=torch.int32, device="cuda"))
+    assert torch.equal(got, one.expand_as(got))
+    pool.close()
