@@ -664,7 +664,13 @@ static void launch_chunk(const LinearArgs& a, const LinearItems& list, hipStream
   if (list.most_parts > 64) launch_scan<16, 8>(a, list, D, s);
   else if (list.most_parts > 32) launch_scan<4, 16>(a, list, D, s);
   else if (list.most_parts > 0) launch_scan<2, 8>(a, list, D, s);
-  hipLaunchKernelGGL(linear_chunk_kernel<D>, dim3(list.n_items * a.Hkv), dim3(2 * D), 0, s, a, list);
+  LinearItems some = list;
+  const int most = (1 << 23) / a.Hkv;  // a launch has fewer than 2^32 threads
+  for (int i = 0; i < list.n_items; i += most) {
+    some.items = list.items + i;
+    some.n_items = std::min(most, list.n_items - i);
+    hipLaunchKernelGGL(linear_chunk_kernel<D>, dim3(some.n_items * a.Hkv), dim3(2 * D), 0, s, a, some);
+  }
 }
 
 hipError_t launch_linear_chunk(const LinearArgs& a, const LinearItems& list, int D, hipStream_t s) {

@@ -182,3 +182,24 @@ def test_append_rope_refuses_more_heads_than_its_indices_hold():
     one = kp.kvp_rope_apply(kp.Rope(64), torch.ones_like(q[:, :1]), torch.tensor([3], dtype=torch.int32, device="cuda"))
     assert torch.equal(got, one.expand_as(got))
     pool.close()
+
+
+def test_linear_more_sequences_than_one_launch_holds():
+    """70000 sequences of 128 heads, 211 of them with a token: out = scale (q . k) v."""
+    import torch
+    note("linear many sequences")
+    B, H, d = 70000, 128, 64
+    lens = np.zeros(B, np.int32)
+    lens[np.random.default_rng(2).choice(B, 210, replace=False)] = 1
+    lens[-1] = 1
+    cu = np.concatenate([[0], np.cumsum(lens)]).astype(np.int32)
+    T = int(cu[-1])
+    g = torch.Generator().manual_seed(3)
+    q, k, v = (torch.randn(T, H, d, generator=g).to(torch.bfloat16).cuda() for _ in range(3))
+    state = torch.zeros(1, H, d, d, device="cuda")
+    none = np.full(B, -1, np.int32)
+    out = kp.linear_chunk_attn(q, k, v, state, np.full(H, 0.5), none, none, cu, scale=0.25, out_dtype=torch.float32)
+    a, b, c = (t.cpu().double().numpy() for t in (q, k, v))
+    want = 0.25 * (a * b).sum(-1, keepdims=True) * c
+    room = 0.25 * (np.abs(a) * np.abs(b)).sum(-1, keepdims=True) * np.abs(c)
+    assert np.all(np.abs(out.cpu().double().numpy() - want) <= 2.0 ** -24 * np.abs(want) + 2.0 ** -16 * room)
