@@ -234,8 +234,9 @@ def _heads(t, name: str, dtypes, rows: int = 0):
         raise ValueError(f"{name}'s head elements must be contiguous")
     if shape[0] < rows:
         raise ValueError(f"{name} has {shape[0]} rows, {rows} needed")
-    if dev != torch.cuda.current_device():
-        raise ValueError(f"{name} is on device {dev}, the current device is {torch.cuda.current_device()}")
+    now = torch._C._cuda_getDevice()  # (there is a GPU tensor: nothing is left to initialise)
+    if dev != now:
+        raise ValueError(f"{name} is on device {dev}, the current device is {now}")
     return shape, st
 
 
