@@ -251,15 +251,18 @@ __global__ __launch_bounds__(256) void gather_kernel(GatherArgs a) {
   }
 }
 
-// kv_append_rope.  One wave per (page run, KV head) turns the keys and writes both blocks; one per (page run, up to
-// kQueryHeads query heads) turns the queries of the same tokens.  A lane holds a unit of 8 dims of one token (in the half
-// layout 8 more, R / 2 further or the next ones that are not rotated), computes its sines and cosines once and uses them
-// for all of the wave's heads; a run of few tokens spreads the heads over the lanes.  Bandwidth is what bounds it: 16416
-// tokens of 32 + 4 heads of 128 (336 MB) take 74 us, 4.5 TB/s of the 5.1 that a copy reaches; 3567 tokens into FP8 pages
-// 16.7 us, 4.2 TB/s.  Waves of 4 query heads: 72 and 15.4 us there, but 24 instead of 21 us for 4160 tokens of 32 + 8
-// heads, and 1.6% more over 36 shapes.  A step of 512 single tokens (11 us) waits for its run records, which lie in pinned
-// host memory, then for page ids, then for rows.
-constexpr int kQueryHeads = 8;
+// kv_append_rope.  One wave per (page run, KV head) turns the keys and writes both blocks; one per (page run, some query
+// heads) turns the queries of the same tokens.  A lane holds a unit of 8 dims of one token (in the half layout 8 more,
+// R / 2 further or the next ones that are not rotated), computes its sines and cosines once and uses them for all of the
+// wave's heads; a run of few tokens spreads the heads over the lanes.  Bandwidth is what bounds it: 16416 tokens of 32 + 4
+// heads of 128 (336 MB) take 74 us, 4.5 TB/s of the 5.1 that a copy reaches; 3567 tokens into FP8 pages 15.4 us, 4.5 TB/s.
+// A step of 512 single tokens (11 us) waits for its run records, which lie in pinned host memory, then for page ids, then
+// for rows.
+//
+// Query heads of a wave: 8, or 4 in the interleaved layout (whose waves take twice the passes over a run) where the waves
+// of a call have room beside each other.  4160 tokens with 8 / 4: 32 + 2 heads interleaved 18.1 / 17.0 us, 8 + 8 17.0 /
+// 15.0; 32 + 8 heads 19.8 / 21.3, not interleaved 20.9 / 23.9; FP8 with 2 for the 3567 tokens 17.2.
+constexpr int kQueryHeads = 8, kFewQueryHeads = 4, kFewWaves = 4096;
 
 template <int D, bool F8, bool IL>
 __global__ __launch_bounds__(256) void append_rope_kernel(AppendRopeArgs r) {
@@ -282,7 +285,7 @@ __global__ __launch_bounds__(256) void append_rope_kernel(AppendRopeArgs r) {
   const int width = ntok * units > 32 ? 64 : ntok * units > 16 ? 32 : ntok * units > 8 ? 16 : 8;
 
   if (!key) {
-    const int h_lo = slot * kQueryHeads, h_hi = min(h_lo + kQueryHeads, r.Hq);
+    const int h_lo = slot * r.q_heads, h_hi = min(h_lo + r.q_heads, r.Hq);
     const int across = 64 / width;  // heads at a time
     for (int e = lane & (width - 1); e < ntok * units; e += width) {
       const int tt = e / units, u = e % units;
@@ -461,9 +464,12 @@ hipError_t launch_append(const AppendArgs& a, int D, hipStream_t s) {
 template <int D, bool F8>
 static void launch_append_rope(const AppendRopeArgs& a, hipStream_t s) {
   const bool whole = a.table.rotary_dim % (a.table.interleaved ? 8 : 16) == 0;
-  const int q_slots = whole ? (a.Hq + kQueryHeads - 1) / kQueryHeads : a.Hq, slots = a.kv.Hkv + q_slots;
+  const int64_t waves = (int64_t)a.kv.n_runs * (a.kv.Hkv + (a.Hq + kFewQueryHeads - 1) / kFewQueryHeads);
+  const int q_heads = !whole ? 1 : a.table.interleaved && waves <= kFewWaves ? kFewQueryHeads : kQueryHeads;
+  const int q_slots = (a.Hq + q_heads - 1) / q_heads, slots = a.kv.Hkv + q_slots;
   const int most = (int)((1u << 30) / slots);  // runs of a launch: 31-bit unit indices
   AppendRopeArgs b = a;
+  b.q_heads = q_heads;
   b.by_slots = FastDiv(slots);
   b.by_keys = FastDiv(a.kv.Hkv);
   b.by_queries = FastDiv(std::max(1, q_slots));

@@ -76,7 +76,8 @@ struct AppendRopeArgs {
   int64_t q_stride, q_out_stride;
   int Hq;
   FastDiv by_slots, by_keys, by_queries;  // of a wave's index (these and q_units: set by launch_append_rope)
-  uint32_t q_units;         // waves for queries
+  uint32_t q_units;         // waves for queries, of q_heads each
+  int q_heads;
 };
 
 // Linear attention over states [slots, Hkv, D, D].  One item is a run of tokens of one sequence.
