@@ -203,3 +203,78 @@ def test_linear_more_sequences_than_one_launch_holds():
     want = 0.25 * (a * b).sum(-1, keepdims=True) * c
     room = 0.25 * (np.abs(a) * np.abs(b)).sum(-1, keepdims=True) * np.abs(c)
     assert np.all(np.abs(out.cpu().double().numpy() - want) <= 2.0 ** -24 * np.abs(want) + 2.0 ** -16 * room)
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("seqs", [200, 270])  # 4 and 8 query heads a wave, interleaved
+@pytest.mark.parametrize("Hq", [32, 40])
+def test_append_rope_of_many_runs(interleaved, seqs, Hq):
+    import torch
+    note(f"append rope many {interleaved} {seqs} {Hq}")
+    Hkv, d = 8, 64
+    g = torch.Generator().manual_seed(seqs)
+    start = np.arange(seqs, dtype=np.int32) * 7
+    new = np.where(np.arange(seqs) % 9 == 0, 17, 1)
+    cu = np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+    T = int(cu[-1])
+    pos = torch.from_numpy(np.concatenate([np.arange(s, s + n) for s, n in zip(start, new)]).astype(np.int32)).cuda()
+    q, k, v = (torch.randn(T, h, d, generator=g).to(torch.bfloat16).cuda() for h in (Hq, Hkv, Hkv))
+    maxp = (int(start[-1]) + 17 + 15) // 16
+    bt = torch.full((seqs, maxp), -1, dtype=torch.int32)
+    pages = 0
+    for i in range(seqs):
+        for p in range(start[i] // 16, (start[i] + new[i] - 1) // 16 + 1):
+            bt[i, p] = pages
+            pages += 1
+    bt = bt.cuda()
+    rope = kp.Rope(32, interleaved=interleaved)
+    a, b = kp.Pool(1, pages, Hkv, d), kp.Pool(1, pages, Hkv, d)
+    got = kp.kv_append_rope(a, 0, rope, k, v, bt, start, cu, q=q)
+    kp.kv_append(b, 0, kp.kvp_rope_apply(rope, k, pos), v, bt, start, cu)
+    assert torch.equal(got, kp.kvp_rope_apply(rope, q, pos))
+    assert torch.equal(a.layer_raw(), b.layer_raw())
+    assert a.device_error() == kp.KVP_OK
+    a.close(), b.close()
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("T,H,d,rot", [(3001, 13, 128, 128), (9001, 30, 128, 64), (20011, 31, 72, 48), (300, 1000, 64, 64)])
+def test_rope_of_large_calls_equals_small_ones(T, H, d, rot, interleaved, dt):
+    """Calls that give a thread two or four heads: the bits of one-head calls, in place and with the gradient's sign."""
+    import torch
+    note(f"rope large calls {T} {H} {d} {rot} {interleaved} {dt}")
+    g = torch.Generator(device="cuda").manual_seed(T)
+    whole = torch.randn(T, H + 3, d, generator=g, device="cuda").to(torch.bfloat16 if dt == "bf16" else torch.float32)
+    x = whole[:, 1:H + 1]
+    pos = torch.randint(-5000, 1 << 20, (T,), generator=g, device="cuda", dtype=torch.int32)
+    rope = kp.Rope(rot, interleaved=interleaved, magnitude=1.25)
+    rest = whole[:, [0, H + 1, H + 2]].clone()
+    want = torch.empty(T, H, d, dtype=x.dtype, device="cuda")
+    for h in range(0, H, max(1, H // 7)):
+        for t in range(0, T, 5000):
+            want[t:t + 5000, h:h + 1] = kp.kvp_rope_apply(rope, x[t:t + 5000, h:h + 1], pos[t:t + 5000], grad=True)
+    got = kp.kvp_rope_apply(rope, x, pos, grad=True)
+    heads = list(range(0, H, max(1, H // 7)))
+    assert torch.equal(got[:, heads], want[:, heads])
+    kp.kvp_rope_apply(rope, x, pos, out=x, grad=True)
+    assert torch.equal(x, got) and torch.equal(whole[:, [0, H + 1, H + 2]], rest)
+
+
+@pytest.mark.parametrize("lens,Hq,Hkv,d", [([100, 60, 7], 16, 1, 128), ([128, 1], 64, 4, 64), ([300, 300, 300], 32, 2, 64)])
+def test_linear_in_place_every_time_the_same(lens, Hq, Hkv, d):
+    """Workgroups that share a sequence's query heads all read the state that one of them replaces."""
+    import torch
+    note(f"linear in place {lens} {Hq}/{Hkv} {d}")
+    c = Case(lens, Hq, Hkv, d)
+    i = list(range(len(lens)))
+    before = c.state.clone()
+    want, room = c.oracle(i, i, d ** -0.5)
+    first = None
+    for rep in range(25):
+        c.state.copy_(before)
+        out = kp.linear_chunk_attn(c.q, c.k, c.v, c.state, c.decay, i, i, c.cu)
+        if first is None:
+            first = out, c.state.clone()
+            check(out, c.state, want, room, c, i)
+        assert torch.equal(out, first[0]) and torch.equal(c.state, first[1])
