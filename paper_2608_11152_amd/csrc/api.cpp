@@ -1171,10 +1171,15 @@ int linear_decode_attn(const void* q, int64_t q_stride, const void* k, int64_t k
                                         out, out_dtype);
   kvp::LinearBatch batch;
   std::memcpy(batch.decay, decay, sizeof(float) * num_kv_heads);
+  batch.few = num_slots <= INT16_MAX + 1;
+  const int most = batch.few ? 2 * kvp::kLinearBatch : kvp::kLinearBatch;
   hipError_t e = hipSuccess;
-  for (int i = 0; i < num_seqs && e == hipSuccess; i += kvp::kLinearBatch) {
-    const int n = std::min(kvp::kLinearBatch, num_seqs - i);
-    for (int j = 0; j < n; ++j) batch.slots[j] = make_int2(src_slots[i + j], dst_slots[i + j]);
+  for (int i = 0; i < num_seqs && e == hipSuccess; i += most) {
+    const int n = std::min(most, num_seqs - i);
+    for (int j = 0; j < n; ++j) {
+      if (batch.few) batch.few_slots[j] = make_short2((short)src_slots[i + j], (short)dst_slots[i + j]);
+      else batch.slots[j] = make_int2(src_slots[i + j], dst_slots[i + j]);
+    }
     batch.first = i;
     e = kvp::launch_linear_decode(a, batch, n, head_dim, reinterpret_cast<hipStream_t>(stream));
   }

@@ -87,13 +87,18 @@ struct LinearItem {
   int32_t g0, gn;           // query heads of the KV head's: first, number
 };
 
-// linear_decode_attn: slots (source, destination) of up to kLinearBatch sequences and the heads' decay, in the launch
-// arguments (4 KB at most), so that no host memory is read later.
+// linear_decode_attn: slots (source, destination) of up to kLinearBatch sequences, twice as many where 16 bits hold every
+// slot, and the heads' decay, in the launch arguments (4 KB at most), so that no host memory is read later.
 constexpr int kLinearBatch = 320, kLinearHeads = 128;
 struct LinearBatch {
-  int2 slots[kLinearBatch];
+  union {
+    int2 slots[kLinearBatch];
+    short2 few_slots[2 * kLinearBatch];
+  };
   float decay[kLinearHeads];
   int32_t first;            // token of slots[0]
+  int32_t few;
+  LinearBatch() {}
 };
 
 // A sequence cut into n parts of len tokens (the last may be shorter): slots part .. part + n - 1 of the workspace.

@@ -582,7 +582,7 @@ __global__ __launch_bounds__(256) void linear_scan_kernel(LinearArgs a, LinearIt
 // Single tokens: one workgroup per (sequence, KV head).  A thread holds 4 columns of D / R rows of the state, R apart, all
 // loads issued before the first is used; the rows' sums for the output meet in the wave and then in LDS.  Bandwidth is
 // what bounds it: the state is read and written once, past the caches.  512 samples of 64 prompts with 16 heads of 128
-// (612 MB, 537 of them written): 133 us in two launches, 4.6 TB/s.  4 sequences: 4.5 us of a call's 13.5.
+// (612 MB, 537 of them written): 128 us, 4.8 TB/s (133 as 320 + 192 sequences).  4 sequences: 4.5 us of a call's 13.5.
 template <int D>
 __global__ __launch_bounds__(256) void linear_token_kernel(LinearArgs a, LinearBatch batch) {
   constexpr int C = D / 4, R = 256 / C, N = D / R;  // threads per row, rows at a time, rows per thread
@@ -592,7 +592,7 @@ __global__ __launch_bounds__(256) void linear_token_kernel(LinearArgs a, LinearB
   const int tid = threadIdx.x, w = tid >> 6, c = 4 * (tid % C), r0 = tid / C;
   const int i = blockIdx.x / a.Hkv, h = blockIdx.x - i * a.Hkv, G = a.Hq / a.Hkv;
   float* const part = qs + G * D;  // [G][4][D]
-  const int src = batch.slots[i].x, dst = batch.slots[i].y;
+  const int src = batch.few ? batch.few_slots[i].x : batch.slots[i].x, dst = batch.few ? batch.few_slots[i].y : batch.slots[i].y;
   const int64_t t = batch.first + i;
   f32x4 S[N] = {};
   if (src >= 0) {

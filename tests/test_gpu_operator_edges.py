@@ -278,3 +278,27 @@ def test_linear_in_place_every_time_the_same(lens, Hq, Hkv, d):
             first = out, c.state.clone()
             check(out, c.state, want, room, c, i)
         assert torch.equal(out, first[0]) and torch.equal(c.state, first[1])
+
+
+@pytest.mark.parametrize("slots", [1300, 32768, 32769, 40000])
+def test_linear_decode_slots_of_16_bits_and_more(slots):
+    """1290 sequences in several launches; the first and the last slots among them."""
+    import torch
+    note(f"linear decode slots {slots}")
+    B, Hq, Hkv, d = 1290, 2, 1, 64
+    c = Case([1] * B, Hq, Hkv, d, slots=4)
+    rng = np.random.default_rng(slots)
+    state = torch.zeros(slots, Hkv, d, d, device="cuda")
+    used = rng.permutation(np.concatenate([[0, slots - 1], 1 + rng.choice(slots - 2, B - 2, replace=False)]))
+    src, dst = used.copy(), used.copy()
+    src[::7], dst[3::11] = -1, -1
+    at = torch.from_numpy(used).cuda()
+    state[at] = torch.randn(B, Hkv, d, d, generator=torch.Generator().manual_seed(1)).cuda()
+    c.state = state[at].clone()
+    small = [np.where(s < 0, -1, np.arange(B)) for s in (src, dst)]
+    want, room = c.oracle(*small, 0.5)
+    untouched = torch.ones(slots, dtype=torch.bool, device="cuda")
+    untouched[at] = False
+    out = kp.linear_decode_attn(c.q, c.k, c.v, state, c.decay, src, dst, scale=0.5)
+    check(out, state[at], want, room, c, small[1])
+    assert not bool(state[untouched].any())
