@@ -581,8 +581,10 @@ __global__ __launch_bounds__(256) void linear_scan_kernel(LinearArgs a, LinearIt
 
 // Single tokens: one workgroup per (sequence, KV head).  A thread holds 4 columns of D / R rows of the state, R apart, all
 // loads issued before the first is used; the rows' sums for the output meet in the wave and then in LDS.  Bandwidth is
-// what bounds it: the state is read and written once, past the caches.  512 samples of 64 prompts with 16 heads of 128
-// (612 MB, 537 of them written): 128 us, 4.8 TB/s (133 as 320 + 192 sequences).  4 sequences: 4.5 us of a call's 13.5.
+// what bounds it: the state is read once and written once, past the caches (ordinary stores: 142 us below).  512 samples
+// of 64 prompts with 16 heads of 128 (612 MB, 537 of them written; a prompt's states are read by its samples from the
+// caches): 106 us, 5.8 TB/s; with streaming loads 128, as 320 + 192 sequences 133.  512 sequences in place (1.07 GB): 182
+// us, 5.9 TB/s; with streaming loads 201.  4 sequences: 4.5 us of a call's 13.5.
 template <int D>
 __global__ __launch_bounds__(256) void linear_token_kernel(LinearArgs a, LinearBatch batch) {
   constexpr int C = D / 4, R = 256 / C, N = D / R;  // threads per row, rows at a time, rows per thread
@@ -598,7 +600,7 @@ __global__ __launch_bounds__(256) void linear_token_kernel(LinearArgs a, LinearB
   if (src >= 0) {
     const float* from = state_at(a, src, h, D) + r0 * D + c;
 #pragma unroll
-    for (int n = 0; n < N; ++n) S[n] = __builtin_nontemporal_load(reinterpret_cast<const f32x4*>(from + n * R * D));
+    for (int n = 0; n < N; ++n) S[n] = *reinterpret_cast<const f32x4*>(from + n * R * D);
   }
   if (tid < D) ks[tid] = widen(a.k[t * a.k_stride + h * D + tid]);
   for (int e = tid; e < G * D; e += 256) qs[e] = widen(a.q[t * a.q_stride + h * G * D + e]);
