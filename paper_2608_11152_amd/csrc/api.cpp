@@ -1004,6 +1004,7 @@ int kv_append_rope(kvp_pool_t pool, int layer, const kvp_rope* rope, const void*
   a.q_stride = q_stride;
   a.q_out_stride = q_out_stride;
   a.Hq = q ? num_q_heads : 0;
+  a.tokens = cu_new[num_seqs];
   e = kvp::launch_append_rope(a, pool->head_dim, s);
   const int rr = staging().release(lease, e == hipSuccess);
   if (e != hipSuccess) return hip_err(e, "kv_append_rope launch");

@@ -255,7 +255,7 @@ __global__ __launch_bounds__(256) void gather_kernel(GatherArgs a) {
 // heads) turns the queries of the same tokens.  A lane holds a unit of 8 dims of one token (in the half layout 8 more,
 // R / 2 further or the next ones that are not rotated), computes its sines and cosines once and uses them for all of the
 // wave's heads; a run of few tokens spreads the heads over the lanes.  Bandwidth is what bounds it: 16416 tokens of 32 + 4
-// heads of 128 (336 MB) take 74 us, 4.5 TB/s of the 5.1 that a copy reaches; 3567 tokens into FP8 pages 15.4 us, 4.5 TB/s.
+// heads of 128 (336 MB) take 64 us, 5.3 TB/s where a copy reaches 5.1; 3567 tokens into FP8 pages 15.4 us, 4.5 TB/s.
 // A step of 512 single tokens (11 us) waits for its run records, which lie in pinned host memory, then for page ids, then
 // for rows.
 //
@@ -264,7 +264,7 @@ __global__ __launch_bounds__(256) void gather_kernel(GatherArgs a) {
 // 15.0; 32 + 8 heads 19.8 / 21.3, not interleaved 20.9 / 23.9; FP8 with 2 for the 3567 tokens 17.2.
 constexpr int kQueryHeads = 8, kFewQueryHeads = 4, kFewWaves = 4096;
 
-template <int D, bool F8, bool IL>
+template <int D, bool F8, bool IL, bool Stream>
 __global__ __launch_bounds__(256) void append_rope_kernel(AppendRopeArgs r) {
   __shared__ uint16_t vstage[4][16 * D];
   const AppendArgs& a = r.kv;
@@ -302,8 +302,8 @@ __global__ __launch_bounds__(256) void append_rope_kernel(AppendRopeArgs r) {
 #pragma unroll
         for (int n = 0; n < N; ++n)
           if (h + n * across < h_hi) {
-            p[n].load(x + (h + n * across) * D);
-            if (!IL) q[n].load(x + (h + n * across) * D + next);
+            p[n].template load<Stream>(x + (h + n * across) * D);
+            if (!IL) q[n].template load<Stream>(x + (h + n * across) * D + next);
           }
 #pragma unroll
         for (int n = 0; n < N; ++n)
@@ -343,8 +343,9 @@ __global__ __launch_bounds__(256) void append_rope_kernel(AppendRopeArgs r) {
   constexpr int CH = D / 8;
   for (int e = lane; e < ntok * CH; e += 64) {
     const int tt = e / CH, c8 = e - tt * CH;
-    *reinterpret_cast<uint4*>(vs + (pr.s_lo + tt) * D + c8 * 8) =
-        *reinterpret_cast<const uint4*>(a.v + (pr.src0 + tt) * r.v_stride + slot * D + c8 * 8);
+    const Eight::u32x4* const at =
+        reinterpret_cast<const Eight::u32x4*>(a.v + (pr.src0 + tt) * r.v_stride + slot * D + c8 * 8);
+    *reinterpret_cast<Eight::u32x4*>(vs + (pr.s_lo + tt) * D + c8 * 8) = Stream ? __builtin_nontemporal_load(at) : *at;
   }
   for (int e = lane; e < ntok * units; e += 64) {
     const int tt = e / units, u = e % units, s = pr.s_lo + tt;
@@ -352,8 +353,8 @@ __global__ __launch_bounds__(256) void append_rope_kernel(AppendRopeArgs r) {
     const bool pass = u >= turned;
     const int i0 = IL ? 8 * u : pass ? 16 * u : 8 * u, next = pass ? 8 : R / 2;
     Eight p, q;
-    p.load(x + i0);
-    if (!IL) q.load(x + i0 + next);
+    p.template load<Stream>(x + i0);
+    if (!IL) q.template load<Stream>(x + i0 + next);
     if (!pass) {
       Turns<IL ? 4 : 8> t;
       t.set(r.table, IL ? u * 4 : u * 8, pr.lpage * 16 + s);
@@ -469,6 +470,8 @@ static void launch_append_rope(const AppendRopeArgs& a, hipStream_t s) {
   const int q_slots = (a.Hq + q_heads - 1) / q_heads, slots = a.kv.Hkv + q_slots;
   const int most = (int)((1u << 30) / slots);  // runs of a launch: 31-bit unit indices
   AppendRopeArgs b = a;
+  // Rows read streamed: 201 MB of them 86 -> 77 us, 151 MB 57 -> 57, 100 MB 40 -> 44 us.
+  const bool stream = a.tokens * (a.Hq + 2 * a.kv.Hkv) * D * 2 >= kStreamBytes;
   b.q_heads = q_heads;
   b.by_slots = FastDiv(slots);
   b.by_keys = FastDiv(a.kv.Hkv);
@@ -479,8 +482,10 @@ static void launch_append_rope(const AppendRopeArgs& a, hipStream_t s) {
     b.q_units = (unsigned)b.kv.n_runs * q_slots;
     const dim3 grid((unsigned)(((int64_t)b.kv.n_runs * slots + 3) / 4));
     if (!whole) hipLaunchKernelGGL((append_rope_pair_kernel<D, F8>), grid, dim3(256), 0, s, b);
-    else if (a.table.interleaved) hipLaunchKernelGGL((append_rope_kernel<D, F8, true>), grid, dim3(256), 0, s, b);
-    else hipLaunchKernelGGL((append_rope_kernel<D, F8, false>), grid, dim3(256), 0, s, b);
+    else if (stream && a.table.interleaved) hipLaunchKernelGGL((append_rope_kernel<D, F8, true, true>), grid, dim3(256), 0, s, b);
+    else if (stream) hipLaunchKernelGGL((append_rope_kernel<D, F8, false, true>), grid, dim3(256), 0, s, b);
+    else if (a.table.interleaved) hipLaunchKernelGGL((append_rope_kernel<D, F8, true, false>), grid, dim3(256), 0, s, b);
+    else hipLaunchKernelGGL((append_rope_kernel<D, F8, false, false>), grid, dim3(256), 0, s, b);
   }
 }
 

@@ -75,6 +75,7 @@ struct AppendRopeArgs {
   uint16_t* q_out;
   int64_t q_stride, q_out_stride;
   int Hq;
+  int64_t tokens;           // of the call
   FastDiv by_slots, by_keys, by_queries;  // of a wave's index (these and q_units: set by launch_append_rope)
   uint32_t q_units;         // waves for queries, of q_heads each
   int q_heads;

@@ -47,9 +47,9 @@ __global__ __launch_bounds__(256) void rope_pair_kernel(RopeArgs a) {
 // A head in units of 8 dims, 16 bytes of bf16 a load: in the half layout a unit and the one R / 2 further, in the
 // interleaved one a unit alone; dims that are not rotated follow.  A thread holds one unit of up to N heads of a token,
 // whose sines and cosines (35 instructions a pair) it computes once, while the loads are under way.  16384 tokens of 36
-// heads of 128, bf16 (302 MB): 64 us, 4.75 TB/s of the 5.1 that a copy reaches; 5003 tokens of 32 heads, fp32, half of
-// each head rotated (164 MB): 33 us, 5.0 TB/s.
-template <class T, bool IL, int N>
+// heads of 128, bf16 (302 MB): 55 us, 5.5 TB/s where a copy reaches 5.1; 5003 tokens of 32 heads, fp32, half of each head
+// rotated (164 MB): 31 us, 5.2 TB/s.
+template <class T, bool IL, int N, bool Stream>
 __global__ __launch_bounds__(256) void rope_unit_kernel(RopeArgs a) {
   const int R = a.table.rotary_dim, turned = IL ? R / 8 : R / 16;
   const unsigned e = blockIdx.x * 256u + threadIdx.x;
@@ -64,8 +64,8 @@ __global__ __launch_bounds__(256) void rope_unit_kernel(RopeArgs a) {
 #pragma unroll
   for (int n = 0; n < N; ++n)
     if (h0 + n * step < a.heads) {
-      p[n].load(x + n * step * a.x_head + i0);
-      if (!IL && !pass) q[n].load(x + n * step * a.x_head + i1);
+      p[n].template load<Stream>(x + n * step * a.x_head + i0);
+      if (!IL && !pass) q[n].template load<Stream>(x + n * step * a.x_head + i1);
     }
   if (!pass) {
     Turns<IL ? 4 : 8> w;
@@ -82,8 +82,8 @@ __global__ __launch_bounds__(256) void rope_unit_kernel(RopeArgs a) {
 #pragma unroll
   for (int n = 0; n < N; ++n)
     if (h0 + n * step < a.heads) {
-      p[n].store(y + n * step * a.y_head + i0);
-      if (!IL && !pass) q[n].store(y + n * step * a.y_head + i1);
+      p[n].template store<Stream>(y + n * step * a.y_head + i0);
+      if (!IL && !pass) q[n].template store<Stream>(y + n * step * a.y_head + i1);
     }
 }
 
@@ -95,7 +95,7 @@ bool in_units(const RopeArgs& a) {
          (reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.y)) % 16 == 0;
 }
 
-template <class T, bool IL, int N>
+template <class T, bool IL, int N, bool Stream = false>
 void launch_units(RopeArgs a, unsigned units, hipStream_t s) {
   a.by_units = FastDiv(units);
   a.by_heads = FastDiv((a.heads + N - 1) / N);
@@ -107,7 +107,7 @@ void launch_units(RopeArgs a, unsigned units, hipStream_t s) {
     b.x = reinterpret_cast<const T*>(a.x) + t * a.x_token;
     b.y = reinterpret_cast<T*>(a.y) + t * a.y_token;
     b.pos = a.pos + t;
-    hipLaunchKernelGGL((rope_unit_kernel<T, IL, N>), dim3((unsigned)((b.tokens * per + 255) / 256)), dim3(256), 0, s, b);
+    hipLaunchKernelGGL((rope_unit_kernel<T, IL, N, Stream>), dim3((unsigned)((b.tokens * per + 255) / 256)), dim3(256), 0, s, b);
   }
 }
 
@@ -118,8 +118,16 @@ void launch_layout(const RopeArgs& a, hipStream_t s) {
   // registers.  36 heads of 128, with 1 / 2 / 4 heads a thread: bf16, 512 tokens (147456 units) 4.9 / 5.1 / 5.8 us, 1024
   // 7.3 / 6.9 / 7.2 us, 16384 interleaved 65 / 57 / 55 us; fp32, 16384 106 / 107 / 113 us.
   const int64_t threads = a.tokens * a.heads * units;
-  if (sizeof(T) == 2 && threads >= 1 << 21 && a.heads >= 4) launch_units<T, IL, sizeof(T) == 2 ? 4 : 2>(a, units, s);
-  else if (threads >= 1 << 18 && a.heads >= 2) launch_units<T, IL, 2>(a, units, s);
+  // Streaming a large call's rows: those 16384 tokens 64 -> 55 us, in a chain with a copy before and one behind 181 -> 156 us
+  // (8192 tokens, 75 MB: 78 -> 81 us; fp32, whose lanes write half of their 32 bytes at a time, 107 -> 132 us).
+  if constexpr (sizeof(T) == 2) {
+    if (threads >= 1 << 21 && a.heads >= 4) {
+      if (a.tokens * a.heads * a.D * (int64_t)sizeof(T) >= kStreamBytes) launch_units<T, IL, 4, true>(a, units, s);
+      else launch_units<T, IL, 4>(a, units, s);
+      return;
+    }
+  }
+  if (threads >= 1 << 18 && a.heads >= 2) launch_units<T, IL, 2>(a, units, s);
   else launch_units<T, IL, 1>(a, units, s);
 }
 

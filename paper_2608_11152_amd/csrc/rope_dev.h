@@ -50,22 +50,27 @@ struct Turns {
   }
 };
 
+// Calls whose rows read are half of the last-level cache (256 MB) or more stream them past the caches.
+constexpr int64_t kStreamBytes = 128ll << 20;
+
 __device__ __forceinline__ float widen(uint16_t b) { return __uint_as_float((unsigned)b << 16); }
 __device__ __forceinline__ uint16_t narrow(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }  // to nearest even
-
 
 // 8 consecutive elements of a head, as bf16 or fp32.
 struct Eight {
   float x[8];
+  typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+  template <bool Stream = false>  // past the caches
   __device__ __forceinline__ void load(const uint16_t* p) {
-    typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
-    const u32x4 v = *reinterpret_cast<const u32x4*>(p);
+    const u32x4* const at = reinterpret_cast<const u32x4*>(p);
+    const u32x4 v = Stream ? __builtin_nontemporal_load(at) : *at;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       x[2 * j] = __uint_as_float(v[j] << 16);
       x[2 * j + 1] = __uint_as_float(v[j] & 0xffff0000u);
     }
   }
+  template <bool Stream = false>
   __device__ __forceinline__ void load(const float* p) {
     const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
     x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
@@ -77,7 +82,13 @@ struct Eight {
     for (int j = 0; j < 8; ++j) v[j] = (__bf16)x[j];
     return __builtin_bit_cast(uint4, v);
   }
-  __device__ __forceinline__ void store(uint16_t* p) const { *reinterpret_cast<uint4*>(p) = bf16(); }
+  template <bool Stream = false>
+  __device__ __forceinline__ void store(uint16_t* p) const {
+    const u32x4 v = __builtin_bit_cast(u32x4, bf16());
+    if (Stream) __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(p));
+    else *reinterpret_cast<u32x4*>(p) = v;
+  }
+  template <bool Stream = false>
   __device__ __forceinline__ void store(float* p) const {
     reinterpret_cast<float4*>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
     reinterpret_cast<float4*>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);

@@ -302,3 +302,45 @@ def test_linear_decode_slots_of_16_bits_and_more(slots):
     out = kp.linear_decode_attn(c.q, c.k, c.v, state, c.decay, src, dst, scale=0.5)
     check(out, state[at], want, room, c, small[1])
     assert not bool(state[untouched].any())
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("fp8", [False, True])
+def test_append_rope_of_rows_that_are_streamed(interleaved, fp8):
+    """135 MB of rows at a fused projection's stride."""
+    import torch
+    note(f"append rope streamed {interleaved} {fp8}")
+    Hq, Hkv, d = 32, 16, 128
+    start, new = np.asarray([5, 0, 9], np.int32), [4099, 4300, 1]
+    cu = np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+    T = int(cu[-1])
+    g = torch.Generator(device="cuda").manual_seed(4)
+    x = torch.randn(T, Hq + 2 * Hkv, d, generator=g, device="cuda").to(torch.bfloat16)
+    q, k, v = x[:, :Hq], x[:, Hq:Hq + Hkv], x[:, Hq + Hkv:]
+    pos = torch.from_numpy(np.concatenate([np.arange(s, s + n) for s, n in zip(start, new)]).astype(np.int32)).cuda()
+    maxp = 270
+    bt = torch.randperm(3 * maxp, generator=torch.Generator().manual_seed(5)).to(torch.int32).view(3, maxp).cuda()
+    rope = kp.Rope(64, interleaved=interleaved)
+    pools = [kp.Pool(1, 3 * maxp, Hkv, d, dtype=kp.KVP_FP8_E4M3 if fp8 else kp.KVP_BF16) for _ in range(2)]
+    got = kp.kv_append_rope(pools[0], 0, rope, k, v, bt, start, cu, q=q)
+    assert torch.equal(got, kp.kvp_rope_apply(rope, q, pos))
+    for i in range(3):  # the same, sequence by sequence: rows that are not streamed
+        lo, hi = int(cu[i]), int(cu[i + 1])
+        kp.kv_append_rope(pools[1], 0, rope, k[lo:hi], v[lo:hi], bt[i:i + 1], start[i:i + 1], [0, hi - lo])
+    a, b = (p.layer_bytes() if fp8 else p.layer_raw() for p in pools)
+    assert torch.equal(a, b) and bool(a.any())
+    for p in pools:
+        p.close()
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_rope_of_rows_that_are_streamed(interleaved):
+    import torch
+    note(f"rope streamed {interleaved}")
+    T, H, d = 17003, 33, 128
+    x = torch.randn(T, H, d, generator=torch.Generator(device="cuda").manual_seed(6), device="cuda").to(torch.bfloat16)
+    pos = torch.arange(T, dtype=torch.int32, device="cuda") * 7
+    rope = kp.Rope(96, interleaved=interleaved)
+    got = kp.kvp_rope_apply(rope, x, pos)
+    for t in range(0, T, 4000):
+        assert torch.equal(got[t:t + 4000], kp.kvp_rope_apply(rope, x[t:t + 4000], pos[t:t + 4000]))
