@@ -1,6 +1,7 @@
 // Linear attention with a decay per head over a state per session:
 //   S_t = decay S_{t-1} + k_t v_t^T,   o_t = scale q_t^T S_t
-// q, k, v bf16, the state and every sum fp32; the output is rounded once.
+// q, k, v bf16, the state and every sum fp32; the output is rounded once.  How the matrix products take fp32 operands
+// stands at linear_chunk_kernel below.
 //
 // linear_token_kernel: single tokens.
 //
@@ -19,9 +20,11 @@
 // Rows of q, k and v go from memory straight to LDS, past the caches (165 -> 163 and 799 -> 776 us below); K^T and V^T
 // come from there through its transposing reads.
 //
-// Operands that are not bf16 are carried as sums of bf16 parts: S and P as two (2^-18 left: far inside a bf16 output's
-// half step 2^-9), the decayed V that goes into the state as three (2^-26: the state is fp32).  A single part for S and P
-// would take 6% less time, with 2^-9 of the state in every output.
+// Operands that are not bf16 are carried as sums of bf16 parts.  The decayed V that goes into the state is three (2^-26
+// left: the state is fp32).  S and P are three for fp32 outputs, which are then 2^-23 off (2-norm, relative), 2^-18.6 with
+// two; the prompts below take 195 us with three, 185 with two.  For bf16 outputs they are two (2^-18 left, far inside the
+// output's half step 2^-9): three take 178 us instead of 159, and with two one output in 500 is rounded to the other
+// neighbour.  One part for S and P would take 6% less time, with 2^-9 of the state in every output.
 //
 // Three workgroups fit a compute unit (50 KB of LDS; 149 VGPRs, which the sched_barriers and Lane keep them at).  64
 // prompts of 128 .. 1024 tokens with 16 heads of 128, 663 MB: 161 us, 4.1 TB/s of the 5.1 that a copy reaches.  The SIMDs
@@ -99,11 +102,11 @@ __device__ __forceinline__ int later(int at, int y, int x, int z) {
 // Row tile rt (16 rows) sees keys of the halves s <= rt / 2 of a chunk.
 __host__ __device__ constexpr int pair_of(int rt, int s) { return rt < 2 ? rt : 2 * rt - 2 + s; }
 constexpr int kPwsBase = 31;
-constexpr int kWeights = 6 * 2 * 1024;  // two bf16 parts of 6 operands, 16 bytes a lane
+constexpr int weights(int parts) { return 6 * parts * 1024; }  // bf16 parts of 6 operands, 16 bytes a lane
 
-template <int D>
+template <int D, int Parts>
 struct Tiles {
-  unsigned char q[2 * D * kChunk > kWeights ? 2 * D * kChunk : kWeights];  // later the weights
+  unsigned char q[std::max(2 * D * kChunk, weights(Parts))];  // later the weights
   unsigned char k[2 * D * kChunk], v[2 * D * kChunk];
   float pw[2 * kChunk];              // decay^(e - 63), 0 below
   float pws[kChunk + 1 + kPwsBase];  // scale decay^(e - kPwsBase), 0 below
@@ -312,9 +315,11 @@ __global__ __launch_bounds__(2 * D, 3) void linear_sum_kernel(LinearArgs a, Line
       for (int r = 0; r < 4; ++r) to[Wave<D>::state_off(mt, nt, r)] = S[mt][nt][r];
 }
 
-template <int D>
+// F32: fp32 outputs.
+template <int D, bool F32>
 __global__ __launch_bounds__(2 * D, 3) void linear_chunk_kernel(LinearArgs a, LinearItems list) {
-  __shared__ Tiles<D> L;
+  constexpr int Parts = F32 ? 3 : 2;  // bf16 parts of the state and the weights
+  __shared__ Tiles<D, Parts> L;
   constexpr int KS = D / 32, MT = Wave<D>::MT;  // k-steps and row tiles over the dims of k
   const Wave<D> me(a.Hkv);
   const int w = me.w, h = me.h, G = a.Hq / a.Hkv, tid = threadIdx.x;
@@ -367,17 +372,18 @@ __global__ __launch_bounds__(2 * D, 3) void linear_chunk_kernel(LinearArgs a, Li
         for (int rt = 0; rt < 4; ++rt) qf[rt] = ld16(L.q + later<D>(q_at ^ (64 * ks), 0, rt & 1, rt >> 1));
 #pragma unroll
         for (int nt = 0; nt < 2; ++nt) {
-          u32x4 hi, lo;
+          u32x4 sp[Parts];
 #pragma unroll
           for (int b = 0; b < 4; ++b) {
             float x = S[2 * ks + (b >> 1)][nt][2 * (b & 1)], y = S[2 * ks + (b >> 1)][nt][2 * (b & 1) + 1];
-            hi[b] = part(x, y);
-            lo[b] = pack2(x, y);
+#pragma unroll
+            for (int p = 0; p + 1 < Parts; ++p) sp[p][b] = part(x, y);
+            sp[Parts - 1][b] = pack2(x, y);
           }
 #pragma unroll
-          for (int rt = 0; rt < 4; ++rt) O[rt][nt] = mfma16(hi, qf[rt], O[rt][nt]);
+          for (int p = 0; p < Parts; ++p)
 #pragma unroll
-          for (int rt = 0; rt < 4; ++rt) O[rt][nt] = mfma16(lo, qf[rt], O[rt][nt]);
+            for (int rt = 0; rt < 4; ++rt) O[rt][nt] = mfma16(sp[p], qf[rt], O[rt][nt]);
         }
       }
       __builtin_amdgcn_sched_barrier(0);
@@ -387,7 +393,7 @@ __global__ __launch_bounds__(2 * D, 3) void linear_chunk_kernel(LinearArgs a, Li
       }
       // The wave's share of the tiles (rt, jt) of P^T = K Q^T; its rows are keys j = 32 (jt / 2) + 4 (jt % 2) + 8 g + r.
       constexpr int W = D / 32, N = 12 / W;
-      u32x2 weight[N][2];
+      u32x2 weight[N][Parts];
       {
         const Lane l;
         const int k_at = tile_at<D>(8 * (l.m >> 2) + (l.m & 3), l.g), q_at = tile_at<D>(l.m, l.g);
@@ -412,8 +418,9 @@ __global__ __launch_bounds__(2 * D, 3) void linear_chunk_kernel(LinearArgs a, Li
 #pragma unroll
           for (int b = 0; b < 2; ++b) {
             float y0 = P[x][2 * b], y1 = P[x][2 * b + 1];
-            weight[x][0][b] = part(y0, y1);
-            weight[x][1][b] = pack2(y0, y1);
+#pragma unroll
+            for (int p = 0; p + 1 < Parts; ++p) weight[x][p][b] = part(y0, y1);
+            weight[x][Parts - 1][b] = pack2(y0, y1);
           }
         }
       }
@@ -421,13 +428,13 @@ __global__ __launch_bounds__(2 * D, 3) void linear_chunk_kernel(LinearArgs a, Li
 #pragma unroll
       for (int x = 0; x < N; ++x) {
         const int t = w + W * x, rt = t < 4 ? t >> 1 : 2 + ((t - 4) >> 2), jt = t < 4 ? t & 1 : t & 3;
-        unsigned char* const to = L.q + 2048 * pair_of(rt, jt >> 1) + 16 * Lane().lane + 8 * (jt & 1);
-        *reinterpret_cast<u32x2*>(to) = weight[x][0];
-        *reinterpret_cast<u32x2*>(to + 1024) = weight[x][1];
+        unsigned char* const to = L.q + 1024 * Parts * pair_of(rt, jt >> 1) + 16 * Lane().lane + 8 * (jt & 1);
+#pragma unroll
+        for (int p = 0; p < Parts; ++p) *reinterpret_cast<u32x2*>(to + 1024 * p) = weight[x][p];
       }
       all_read();
       me.load_v(L.v, vf);
-      const int es = a.out_f32 ? 4 : 2;
+      const int es = F32 ? 4 : 2;
       char* const out = reinterpret_cast<char*>(a.out) + ((it.t0 + (int64_t)c) * a.Hq + first + gq) * D * es;
       bool bad = false;
 #pragma unroll
@@ -437,12 +444,14 @@ __global__ __launch_bounds__(2 * D, 3) void linear_chunk_kernel(LinearArgs a, Li
         f32x4 V[2] = {};
 #pragma unroll
         for (int s = 0; s <= rt / 2; ++s) {
-          const unsigned char* const from = L.q + 2048 * pair_of(rt, s) + 16 * l.lane;
-          const u32x4 hi = ld16(from), lo = ld16(from + 1024);
+          const unsigned char* const from = L.q + 1024 * Parts * pair_of(rt, s) + 16 * l.lane;
+          u32x4 wp[Parts];
 #pragma unroll
-          for (int nt = 0; nt < 2; ++nt) V[nt] = mfma16(vf[s][nt], hi, V[nt]);
+          for (int p = 0; p < Parts; ++p) wp[p] = ld16(from + 1024 * p);
 #pragma unroll
-          for (int nt = 0; nt < 2; ++nt) V[nt] = mfma16(vf[s][nt], lo, V[nt]);
+          for (int p = 0; p < Parts; ++p)
+#pragma unroll
+            for (int nt = 0; nt < 2; ++nt) V[nt] = mfma16(vf[s][nt], wp[p], V[nt]);
         }
         if (rt == 3) {
           // A value of v that is not finite gives no number in the chunk's last row, and, as 0 times it, in earlier
@@ -488,7 +497,7 @@ __global__ __launch_bounds__(2 * D, 3) void linear_chunk_kernel(LinearArgs a, Li
           for (int r = 0; r < 4; ++r) V[nt][r] = fmaf(O[rt][nt][r], f, V[nt][r]);
         if (i < n) {
           const int at = i * a.Hq * D + 32 * w + 8 * l.g;
-          if (a.out_f32) {
+          if constexpr (F32) {
             f32x4* o = reinterpret_cast<f32x4*>(out + 4 * (int64_t)at);
             o[0] = V[0];
             o[1] = V[1];
@@ -660,7 +669,7 @@ static void launch_scan(const LinearArgs& a, const LinearItems& list, int D, hip
   hipLaunchKernelGGL((linear_scan_kernel<Ways, U>), grid, dim3(256), 0, s, a, list, D);
 }
 
-template <int D>
+template <int D, bool F32>
 static void launch_chunk(const LinearArgs& a, const LinearItems& list, hipStream_t s) {
   if (list.n_sums > 0) hipLaunchKernelGGL(linear_sum_kernel<D>, dim3(list.n_sums * a.Hkv), dim3(2 * D), 0, s, a, list);
   if (list.most_parts > 64) launch_scan<16, 8>(a, list, D, s);
@@ -671,14 +680,14 @@ static void launch_chunk(const LinearArgs& a, const LinearItems& list, hipStream
   for (int i = 0; i < list.n_items; i += most) {
     some.items = list.items + i;
     some.n_items = std::min(most, list.n_items - i);
-    hipLaunchKernelGGL(linear_chunk_kernel<D>, dim3(some.n_items * a.Hkv), dim3(2 * D), 0, s, a, some);
+    hipLaunchKernelGGL((linear_chunk_kernel<D, F32>), dim3(some.n_items * a.Hkv), dim3(2 * D), 0, s, a, some);
   }
 }
 
 hipError_t launch_linear_chunk(const LinearArgs& a, const LinearItems& list, int D, hipStream_t s) {
   if (list.n_items == 0) return hipSuccess;
-  if (D == 128) launch_chunk<128>(a, list, s);
-  else launch_chunk<64>(a, list, s);
+  if (D == 128) a.out_f32 ? launch_chunk<128, true>(a, list, s) : launch_chunk<128, false>(a, list, s);
+  else a.out_f32 ? launch_chunk<64, true>(a, list, s) : launch_chunk<64, false>(a, list, s);
   return hipGetLastError();
 }
 
