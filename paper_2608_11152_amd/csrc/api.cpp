@@ -614,98 +614,6 @@ int check_cu(const int32_t* cu, int num_seqs) {
   return KVP_OK;
 }
 
-// The work of linear_chunk_attn.  Workgroups fit the GPU three to a compute unit, those of head_dim 64 five; a sequence of
-// more than twice an even share of the call's tokens is cut into parts of about that share.  Shares are for three
-// workgroups (131071 tokens of 16 heads of 128: 784 us; for two or four 816 us), at head_dim 64 for four (24 calls take
-// 0.94 of their time with shares for three, 0.96 with five).  Parts go down to single chunks: 24 calls take 0.88 and 0.83
-// of their time with parts of 128 and 64 tokens on, against parts of 256 on.  Cutting takes two more launches and a second
-// pass over k and v, which walking a few chunks is quicker than: about 5 us a chunk for one query head and 3.5 us for each
-// further one.  Uncut / cut, 8 KV heads of 64, one sequence: of 256 tokens 25 / 27 us, 320 tokens 31 / 27 us; with 2 query
-// heads a KV head 192 tokens 31 / 26 us; with 8, 129 tokens 92 / 46 us.
-//
-// Where no more than half of those workgroups would have work, the query heads of a KV head are shared out too, `split`
-// ways; each workgroup walks the state for itself, the first one keeps it.  A sequence whose state is updated in place has
-// it copied first (a part of its own, written by linear_scan_kernel): the others still read what the first one writes.
-// That launch costs as much as one head's chunk or two.  Not split / split, head_dim 128: 16 query heads on one KV head, 6
-// sequences of 85 .. 137 tokens 124 / 24 us; 128 on 8, 8 of 128 tokens 149 / 46 us; 32 on 8, one of 128 in place 39 / 23
-// us, of 64 22 / 22 us.  Filling the GPU twice over is slower: 16 on 8, 93 single tokens 24 us, with twice the workgroups
-// 31 us.
-struct LinearPlan {
-  std::vector<kvp::LinearItem> items, sums;
-  std::vector<kvp::LinearScan> scans;
-  int parts = 0;
-};
-constexpr int kLinearBlocks128 = 3 * 256, kLinearBlocks64 = 4 * 256, kLinearChunk = 64, kLinearMinWork = 512;
-constexpr int kLinearMinCopy = 4, kLinearMaxGroup = 16;
-
-int linear_blocks(int head_dim) { return head_dim == 64 ? kLinearBlocks64 : kLinearBlocks128; }
-
-int64_t linear_share(const int32_t* cu, int num_seqs, int num_kv_heads, int head_dim) {
-  const int blocks = linear_blocks(head_dim);
-  return std::max<int64_t>(kLinearChunk, ((int64_t)cu[num_seqs] * num_kv_heads + blocks - 1) / blocks);
-}
-
-// Parts of a sequence of n tokens, each of *len of them (the last may be shorter).  group: query heads per KV head.
-int linear_parts(int32_t n, int64_t share, int group, int32_t* len) {
-  *len = n;
-  if (n <= 2 * share || (int64_t)n * (1 + group) <= kLinearMinWork) return 1;
-  const int64_t want = (n + share - 1) / share;
-  *len = (int32_t)(((n + want - 1) / want + kLinearChunk - 1) / kLinearChunk * kLinearChunk);
-  return (n + *len - 1) / *len;
-}
-
-// The parts that a call may need, whatever its query heads and slots.
-int64_t linear_most_parts(const int32_t* cu, int num_seqs, int num_kv_heads, int head_dim) {
-  const int64_t share = linear_share(cu, num_seqs, num_kv_heads, head_dim);
-  const bool split = (int64_t)num_seqs * num_kv_heads * 2 <= linear_blocks(head_dim);
-  int64_t parts = 0;
-  for (int i = 0; i < num_seqs; ++i) {
-    int32_t len;
-    const int m = linear_parts(cu[i + 1] - cu[i], share, kLinearMaxGroup, &len);
-    if (m > 1 || (split && len > 0)) parts += m;
-  }
-  return parts;
-}
-
-void plan_linear(const int32_t* cu, int num_seqs, int num_kv_heads, int head_dim, int group, const int32_t* src,
-                 const int32_t* dst, LinearPlan* P) {
-  const int64_t share = linear_share(cu, num_seqs, num_kv_heads, head_dim);
-  int64_t blocks = 0;
-  int32_t len;
-  for (int i = 0; i < num_seqs; ++i) blocks += linear_parts(cu[i + 1] - cu[i], share, group, &len);
-  blocks *= num_kv_heads;
-  int split = 1;
-  while (2 * split <= group && 2 * split * blocks <= linear_blocks(head_dim)) split *= 2;
-  auto add = [&](int32_t t0, int32_t n, int32_t from, int32_t to, int ways) {
-    for (int w = 0; w < ways; ++w) P->items.push_back({t0, n, from, w == 0 ? to : -1, w * (group / ways), group / ways});
-  };
-  for (int i = 0; i < num_seqs; ++i) {
-    const int32_t n = cu[i + 1] - cu[i], from = src[i], to = dst[i];
-    const int m = linear_parts(n, share, group, &len);
-    if (m == 1) {
-      const bool in_place = from >= 0 && from == to;
-      const int chunks = (n + kLinearChunk - 1) / kLinearChunk;
-      const int ways = n == 0 || (in_place && (group - group / split) * chunks < kLinearMinCopy) ? 1 : split;
-      if (in_place && ways > 1) {
-        P->scans.push_back({from, P->parts, 1, n});
-        add(cu[i], n, -2 - P->parts++, to, ways);
-      } else {
-        add(cu[i], n, from, to, ways);
-      }
-      continue;
-    }
-    for (int32_t p = 0; p < m; ++p) {
-      const int32_t t0 = cu[i] + p * len, cnt = std::min(len, n - p * len);
-      add(t0, cnt, p == 0 && from < 0 ? -1 : -2 - (P->parts + p), p + 1 < m ? -1 : to, split);
-      if (p + 1 < m) P->sums.push_back({t0, cnt, -1, -2 - (P->parts + p + 1), 0, 0});
-    }
-    P->scans.push_back({from, P->parts, m, len});
-    P->parts += m;
-  }
-  // longest first: the last workgroups to start are short
-  std::stable_sort(P->items.begin(), P->items.end(), [](const auto& x, const auto& y) { return x.n > y.n; });
-}
-
 static_assert(kvp::kLinearHeads == KVP_LINEAR_MAX_HEADS && kvp::kRopePairs == KVP_ROPE_PAIRS, "as in the header");
 
 constexpr int64_t kLinearMaxStride = 1 << 24;
@@ -747,7 +655,7 @@ int check_linear(const void* q, int64_t q_stride, const void* k, int64_t k_strid
   if (num_kv_heads <= 0 || num_kv_heads > KVP_LINEAR_MAX_HEADS)
     return set_err(KVP_EUNSUPPORTED, "num_kv_heads %d outside [1, %d]", num_kv_heads, KVP_LINEAR_MAX_HEADS);
   const int G = num_q_heads / num_kv_heads;
-  if (num_q_heads <= 0 || num_q_heads % num_kv_heads || G > kLinearMaxGroup || (G & (G - 1)))
+  if (num_q_heads <= 0 || num_q_heads % num_kv_heads || G > kvp::kLinearMaxGroup || (G & (G - 1)))
     return set_err(KVP_EUNSUPPORTED, "num_q_heads / num_kv_heads = %d / %d is not 1, 2, 4, 8 or 16", num_q_heads,
                    num_kv_heads);
   if (out_dtype != KVP_BF16 && out_dtype != KVP_F32) return set_err(KVP_EUNSUPPORTED, "out_dtype %d", out_dtype);
@@ -1102,7 +1010,7 @@ int linear_chunk_workspace_size(const int32_t* cu, int num_seqs, int num_kv_head
   if (num_seqs == 0) return KVP_OK;
   const int rc = check_cu(cu, num_seqs);
   if (rc) return rc;
-  *bytes = (size_t)linear_most_parts(cu, num_seqs, num_kv_heads, head_dim) * num_kv_heads * head_dim * head_dim *
+  *bytes = (size_t)kvp::linear_most_parts(cu, num_seqs, num_kv_heads, head_dim) * num_kv_heads * head_dim * head_dim *
            sizeof(float);
   return KVP_OK;
 } catch (const std::exception& x) {
@@ -1124,8 +1032,8 @@ int linear_chunk_attn(const void* q, int64_t q_stride, const void* k, int64_t k_
   for (const int64_t stride : {q_stride, k_stride, v_stride})  // the kernel reads a chunk's rows at 32-bit offsets
     if (cu[num_seqs] > 0 && (stride < head_dim || stride > kLinearMaxStride))
       return set_err(KVP_EINVAL, "stride %lld outside [head_dim, %lld]", (long long)stride, (long long)kLinearMaxStride);
-  LinearPlan P;
-  plan_linear(cu, num_seqs, num_kv_heads, head_dim, num_q_heads / num_kv_heads, src_slots, dst_slots, &P);
+  kvp::LinearPlan P;
+  kvp::plan_linear(cu, num_seqs, num_kv_heads, head_dim, num_q_heads / num_kv_heads, src_slots, dst_slots, &P);
   const size_t need = (size_t)P.parts * num_kv_heads * head_dim * head_dim * sizeof(float);
   if (need > 0 && (!ws || ws_bytes < need || (reinterpret_cast<uintptr_t>(ws) & 15) != 0))
     return set_err(KVP_EWORKSPACE, "workspace of %zu bytes (16-byte aligned), %zu needed", ws ? ws_bytes : 0, need);

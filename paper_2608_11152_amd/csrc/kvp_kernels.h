@@ -81,13 +81,6 @@ struct AppendRopeArgs {
   int q_heads;
 };
 
-// Linear attention over states [slots, Hkv, D, D].  One item is a run of tokens of one sequence.
-struct LinearItem {
-  int32_t t0, n;            // first token, tokens
-  int32_t src, dst;         // state slots; -1: starts from zeros / is not kept
-  int32_t g0, gn;           // query heads of the KV head's: first, number
-};
-
 // linear_decode_attn: slots (source, destination) of up to kLinearBatch sequences, twice as many where 16 bits hold every
 // slot, and the heads' decay, in the launch arguments (4 KB at most), so that no host memory is read later.
 constexpr int kLinearBatch = 320, kLinearHeads = 128;
@@ -100,11 +93,6 @@ struct LinearBatch {
   int32_t first;            // token of slots[0]
   int32_t few;
   LinearBatch() {}
-};
-
-// A sequence cut into n parts of len tokens (the last may be shorter): slots part .. part + n - 1 of the workspace.
-struct LinearScan {
-  int32_t src, part, n, len;
 };
 
 // linear_chunk_attn: its work, in pinned host memory.  Slots below -1 are parts of long sequences, -2 the first.

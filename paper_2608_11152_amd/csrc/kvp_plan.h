@@ -125,6 +125,47 @@ int64_t prefill_mean_stages(const PrefillPlan& plan);
 Status check_tables(const int32_t* bt, int maxp, const int32_t* lens, int B, int num_pages,
                     const kvp_group_prefix* gp);
 
+// Linear attention over states [slots, Hkv, D, D].  One item is a run of tokens of one sequence.
+struct LinearItem {
+  int32_t t0, n;            // first token, tokens
+  int32_t src, dst;         // state slots; -1: starts from zeros / is not kept
+  int32_t g0, gn;           // query heads of the KV head's: first, number
+};
+
+// A sequence cut into n parts of len tokens (the last may be shorter): slots part .. part + n - 1 of the workspace.
+struct LinearScan {
+  int32_t src, part, n, len;
+};
+
+// The work of linear_chunk_attn.  Workgroups fit the GPU three to a compute unit, those of head_dim 64 five; a sequence of
+// more than twice an even share of the call's tokens is cut into parts of about that share.  Shares are for three
+// workgroups (131071 tokens of 16 heads of 128: 784 us; for two or four 816 us), at head_dim 64 for four (24 calls take
+// 0.94 of their time with shares for three, 0.96 with five).  Parts go down to single chunks: 24 calls take 0.88 and 0.83
+// of their time with parts of 128 and 64 tokens on, against parts of 256 on.  Cutting takes two more launches and a second
+// pass over k and v, which walking a few chunks is quicker than: about 5 us a chunk for one query head and 3.5 us for each
+// further one.  Uncut / cut, 8 KV heads of 64, one sequence: of 256 tokens 25 / 27 us, 320 tokens 31 / 27 us; with 2 query
+// heads a KV head 192 tokens 31 / 26 us; with 8, 129 tokens 92 / 46 us.
+//
+// Where no more than half of those workgroups would have work, the query heads of a KV head are shared out too, `split`
+// ways; each workgroup walks the state for itself, the first one keeps it.  A sequence whose state is updated in place has
+// it copied first (a part of its own, written by linear_scan_kernel): the others still read what the first one writes.
+// That launch costs as much as one head's chunk or two.  Not split / split, head_dim 128: 16 query heads on one KV head, 6
+// sequences of 85 .. 137 tokens 124 / 24 us; 128 on 8, 8 of 128 tokens 149 / 46 us; 32 on 8, one of 128 in place 39 / 23
+// us, of 64 22 / 22 us.  Filling the GPU twice over is slower: 16 on 8, 93 single tokens 24 us, with twice the workgroups
+// 31 us.
+struct LinearPlan {
+  std::vector<LinearItem> items, sums;
+  std::vector<LinearScan> scans;
+  int parts = 0;
+};
+constexpr int kLinearMaxGroup = 16;
+
+// The parts that a call may need, whatever its query heads and slots.
+int64_t linear_most_parts(const int32_t* cu, int num_seqs, int num_kv_heads, int head_dim);
+// group: query heads per KV head.
+void plan_linear(const int32_t* cu, int num_seqs, int num_kv_heads, int head_dim, int group, const int32_t* src,
+                 const int32_t* dst, LinearPlan* plan);
+
 constexpr int kPrefillWaves = 8;                    // waves per prefill workgroup, 32 query rows each
 constexpr int kPrefillRows = 32 * kPrefillWaves;    // flattened query rows per prefill workgroup
 // A call whose tiles (x their 64-key stages) would not give about this many equal workgroups splits

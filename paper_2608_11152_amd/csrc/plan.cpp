@@ -516,4 +516,78 @@ Status check_tables(const int32_t* bt, int maxp, const int32_t* lens, int B, int
   return {};
 }
 
+namespace {
+
+constexpr int kLinearBlocks128 = 3 * 256, kLinearBlocks64 = 4 * 256, kLinearChunk = 64, kLinearMinWork = 512;
+constexpr int kLinearMinCopy = 4;
+
+int linear_blocks(int head_dim) { return head_dim == 64 ? kLinearBlocks64 : kLinearBlocks128; }
+
+int64_t linear_share(const int32_t* cu, int num_seqs, int num_kv_heads, int head_dim) {
+  const int blocks = linear_blocks(head_dim);
+  return std::max<int64_t>(kLinearChunk, ((int64_t)cu[num_seqs] * num_kv_heads + blocks - 1) / blocks);
+}
+
+// Parts of a sequence of n tokens, each of *len of them (the last may be shorter).  group: query heads per KV head.
+int linear_parts(int32_t n, int64_t share, int group, int32_t* len) {
+  *len = n;
+  if (n <= 2 * share || (int64_t)n * (1 + group) <= kLinearMinWork) return 1;
+  const int64_t want = (n + share - 1) / share;
+  *len = (int32_t)(((n + want - 1) / want + kLinearChunk - 1) / kLinearChunk * kLinearChunk);
+  return (n + *len - 1) / *len;
+}
+
+}  // namespace
+
+int64_t linear_most_parts(const int32_t* cu, int num_seqs, int num_kv_heads, int head_dim) {
+  const int64_t share = linear_share(cu, num_seqs, num_kv_heads, head_dim);
+  const bool split = (int64_t)num_seqs * num_kv_heads * 2 <= linear_blocks(head_dim);
+  int64_t parts = 0;
+  for (int i = 0; i < num_seqs; ++i) {
+    int32_t len;
+    const int m = linear_parts(cu[i + 1] - cu[i], share, kLinearMaxGroup, &len);
+    if (m > 1 || (split && len > 0)) parts += m;
+  }
+  return parts;
+}
+
+void plan_linear(const int32_t* cu, int num_seqs, int num_kv_heads, int head_dim, int group, const int32_t* src,
+                 const int32_t* dst, LinearPlan* P) {
+  const int64_t share = linear_share(cu, num_seqs, num_kv_heads, head_dim);
+  int64_t blocks = 0;
+  int32_t len;
+  for (int i = 0; i < num_seqs; ++i) blocks += linear_parts(cu[i + 1] - cu[i], share, group, &len);
+  blocks *= num_kv_heads;
+  int split = 1;
+  while (2 * split <= group && 2 * split * blocks <= linear_blocks(head_dim)) split *= 2;
+  auto add = [&](int32_t t0, int32_t n, int32_t from, int32_t to, int ways) {
+    for (int w = 0; w < ways; ++w) P->items.push_back({t0, n, from, w == 0 ? to : -1, w * (group / ways), group / ways});
+  };
+  for (int i = 0; i < num_seqs; ++i) {
+    const int32_t n = cu[i + 1] - cu[i], from = src[i], to = dst[i];
+    const int m = linear_parts(n, share, group, &len);
+    if (m == 1) {
+      const bool in_place = from >= 0 && from == to;
+      const int chunks = (n + kLinearChunk - 1) / kLinearChunk;
+      const int ways = n == 0 || (in_place && (group - group / split) * chunks < kLinearMinCopy) ? 1 : split;
+      if (in_place && ways > 1) {
+        P->scans.push_back({from, P->parts, 1, n});
+        add(cu[i], n, -2 - P->parts++, to, ways);
+      } else {
+        add(cu[i], n, from, to, ways);
+      }
+      continue;
+    }
+    for (int32_t p = 0; p < m; ++p) {
+      const int32_t t0 = cu[i] + p * len, cnt = std::min(len, n - p * len);
+      add(t0, cnt, p == 0 && from < 0 ? -1 : -2 - (P->parts + p), p + 1 < m ? -1 : to, split);
+      if (p + 1 < m) P->sums.push_back({t0, cnt, -1, -2 - (P->parts + p + 1), 0, 0});
+    }
+    P->scans.push_back({from, P->parts, m, len});
+    P->parts += m;
+  }
+  // longest first: the last workgroups to start are short
+  std::stable_sort(P->items.begin(), P->items.end(), [](const auto& x, const auto& y) { return x.n > y.n; });
+}
+
 }  // namespace kvp
