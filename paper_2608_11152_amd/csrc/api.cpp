@@ -1034,6 +1034,7 @@ int linear_chunk_attn(const void* q, int64_t q_stride, const void* k, int64_t k_
       return set_err(KVP_EINVAL, "stride %lld outside [head_dim, %lld]", (long long)stride, (long long)kLinearMaxStride);
   kvp::LinearPlan P;
   kvp::plan_linear(cu, num_seqs, num_kv_heads, head_dim, num_q_heads / num_kv_heads, src_slots, dst_slots, &P);
+  if (P.items.empty()) return KVP_OK;  // no tokens, and no state that moves
   const size_t need = (size_t)P.parts * num_kv_heads * head_dim * head_dim * sizeof(float);
   if (need > 0 && (!ws || ws_bytes < need || (reinterpret_cast<uintptr_t>(ws) & 15) != 0))
     return set_err(KVP_EWORKSPACE, "workspace of %zu bytes (16-byte aligned), %zu needed", ws ? ws_bytes : 0, need);

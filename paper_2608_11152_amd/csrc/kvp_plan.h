@@ -153,6 +153,10 @@ struct LinearScan {
 // sequences of 85 .. 137 tokens 124 / 24 us; 128 on 8, 8 of 128 tokens 149 / 46 us; 32 on 8, one of 128 in place 39 / 23
 // us, of 64 22 / 22 us.  Filling the GPU twice over is slower: 16 on 8, 93 single tokens 24 us, with twice the workgroups
 // 31 us.
+//
+// Sequences without tokens are no work: one gets an item only if its state moves to another slot, and they do not count
+// among the workgroups that would have work (64 query heads on 4, one sequence of 128 tokens beside 199 idle ones: 27 us,
+// alone 24; counted, 146).
 struct LinearPlan {
   std::vector<LinearItem> items, sums;
   std::vector<LinearScan> scans;

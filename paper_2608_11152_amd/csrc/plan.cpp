@@ -541,8 +541,9 @@ int linear_parts(int32_t n, int64_t share, int group, int32_t* len) {
 
 int64_t linear_most_parts(const int32_t* cu, int num_seqs, int num_kv_heads, int head_dim) {
   const int64_t share = linear_share(cu, num_seqs, num_kv_heads, head_dim);
-  const bool split = (int64_t)num_seqs * num_kv_heads * 2 <= linear_blocks(head_dim);
-  int64_t parts = 0;
+  int64_t busy = 0, parts = 0;  // sequences with tokens
+  for (int i = 0; i < num_seqs; ++i) busy += cu[i + 1] > cu[i];
+  const bool split = busy * num_kv_heads * 2 <= linear_blocks(head_dim);
   for (int i = 0; i < num_seqs; ++i) {
     int32_t len;
     const int m = linear_parts(cu[i + 1] - cu[i], share, kLinearMaxGroup, &len);
@@ -556,7 +557,8 @@ void plan_linear(const int32_t* cu, int num_seqs, int num_kv_heads, int head_dim
   const int64_t share = linear_share(cu, num_seqs, num_kv_heads, head_dim);
   int64_t blocks = 0;
   int32_t len;
-  for (int i = 0; i < num_seqs; ++i) blocks += linear_parts(cu[i + 1] - cu[i], share, group, &len);
+  for (int i = 0; i < num_seqs; ++i)
+    if (cu[i + 1] > cu[i]) blocks += linear_parts(cu[i + 1] - cu[i], share, group, &len);
   blocks *= num_kv_heads;
   int split = 1;
   while (2 * split <= group && 2 * split * blocks <= linear_blocks(head_dim)) split *= 2;
@@ -565,11 +567,15 @@ void plan_linear(const int32_t* cu, int num_seqs, int num_kv_heads, int head_dim
   };
   for (int i = 0; i < num_seqs; ++i) {
     const int32_t n = cu[i + 1] - cu[i], from = src[i], to = dst[i];
+    if (n == 0) {  // nothing to do, unless its state moves
+      if (to >= 0 && to != from) add(cu[i], 0, from, to, 1);
+      continue;
+    }
     const int m = linear_parts(n, share, group, &len);
     if (m == 1) {
       const bool in_place = from >= 0 && from == to;
       const int chunks = (n + kLinearChunk - 1) / kLinearChunk;
-      const int ways = n == 0 || (in_place && (group - group / split) * chunks < kLinearMinCopy) ? 1 : split;
+      const int ways = in_place && (group - group / split) * chunks < kLinearMinCopy ? 1 : split;
       if (in_place && ways > 1) {
         P->scans.push_back({from, P->parts, 1, n});
         add(cu[i], n, -2 - P->parts++, to, ways);
