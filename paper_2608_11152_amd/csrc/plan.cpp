@@ -534,7 +534,7 @@ int linear_parts(int32_t n, int64_t share, int group, int32_t* len) {
   if (n <= 2 * share || (int64_t)n * (1 + group) <= kLinearMinWork) return 1;
   const int64_t want = (n + share - 1) / share;
   *len = (int32_t)(((n + want - 1) / want + kLinearChunk - 1) / kLinearChunk * kLinearChunk);
-  return (n + *len - 1) / *len;
+  return (n - 1) / *len + 1;
 }
 
 }  // namespace

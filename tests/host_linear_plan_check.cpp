@@ -1,5 +1,5 @@
 // Host-only check of the linear attention planner (plan.cpp), built with g++ and the address and undefined-behaviour
-// sanitizers by tests/test_linear_plan_host.py.  Randomized calls (0 to 2^30 tokens, empty sequences, 1 to 128 KV heads,
+// sanitizers by tests/test_linear_plan_host.py.  Randomized calls (0 to 2^31 - 1 tokens, empty sequences, 1 to 128 KV heads,
 // 1 to 16 query heads each, states in place, forked, fresh and not kept) are planned, and the plan is carried out with a
 // number for a state (every token adds its own) in the order of the launches: sums, scans, items.
 //   - every token of every query head belongs to exactly one item, whose state before it is the sum of its sequence's source
@@ -175,9 +175,9 @@ static Call random_call() {
   for (int i = 0; i < B; ++i) {
     const bool idle = kinds > 0 && between(0, kinds == 1 ? 2 : 20) > 0;
     at += idle ? 0 : between(kinds == 0 ? 1 : 0, hi);
-    c.cu.push_back((int32_t)std::min<int64_t>(at, 1 << 30));
+    c.cu.push_back((int32_t)std::min<int64_t>(at, INT32_MAX));
   }
-  if (between(0, 9) == 0) c.cu.back() = 1 << 30;
+  if (between(0, 9) == 0) c.cu.back() = INT32_MAX;
   c.slots = 2 * B + 1;
   for (int i = 0; i < B; ++i) {
     const int k = (int)between(0, 4);  // in place, fresh, fork, not kept, handed nowhere
