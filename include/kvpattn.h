@@ -328,8 +328,9 @@ int kv_append_rope(kvp_pool_t pool, int layer, const kvp_rope* rope, const void*
  *               the states.  KVP_F32 outputs and the states are computed as in fp32 throughout; for KVP_BF16 ones
  *               linear_chunk_attn holds the state and the weights of a chunk to 2^-18 before the sums, which are fp32
  * Strides are in elements, multiples of 8, and the pointers 16-byte aligned.  head_dim is 64 or 128, num_kv_heads at
- * most KVP_LINEAR_MAX_HEADS, num_q_heads / num_kv_heads 1, 2, 4, 8 or 16.  An infinity or NaN in a token's q, k or v leaves earlier tokens, other heads and other
- * sequences as they are.
+ * most KVP_LINEAR_MAX_HEADS, num_q_heads / num_kv_heads 1, 2, 4, 8 or 16.
+ * An infinity or NaN in a token's q, k or v leaves earlier tokens, other heads and other sequences as they are; earlier
+ * tokens of its head may be rounded another way where it is in v.
  * Errors: KVP_ERANGE for a slot outside [-1, num_slots); KVP_EINVAL for a destination that is another sequence's
  * source or destination, or a decay outside (0, 1]; KVP_EUNSUPPORTED for heads or dtypes not named here.
  * ------------------------------------------------------------------------------------------------- */

@@ -62,3 +62,64 @@ def test_more_items_than_one_launch_holds():
         want = 0.25 * (a * b).sum(-1, keepdim=True) * c
         room = 0.25 * (a.abs() * b.abs()).sum(-1, keepdim=True) * c.abs()
         assert bool(((out[lo:lo + 10000] - want).abs() <= 2.0 ** -16 * room).all())
+
+
+# Values that are not finite.  Tolerance of what must stay: the docstring of test_gpu_linear.py, against the recurrence
+# without the bad value.
+@pytest.mark.parametrize("what", ["q", "k", "v"])
+@pytest.mark.parametrize("value", [float("inf"), float("-inf"), float("nan")])
+@pytest.mark.parametrize("lens,Hq,Hkv,d,at", [
+    ([700, 90], 4, 2, 64, 0), ([700, 90], 4, 2, 64, 337), ([700, 90], 4, 2, 128, 63),   # cut: in and around the parts,
+    ([700, 90], 4, 2, 128, 64), ([700, 90], 4, 2, 64, 128), ([700, 90], 4, 2, 128, 699),  # at their ends
+    ([100, 90], 16, 1, 128, 40), ([100, 90], 16, 1, 64, 99),                             # query heads shared out, in place
+    ([2500], 1, 1, 64, 1300), ([4160], 1, 1, 64, 4000),                                  # the other scans
+])
+def test_bad_values_in_parts_and_shared_out_heads(lens, Hq, Hkv, d, at, what, value):
+    """Nothing but the bad token and, through the state, later tokens of its head and sequence changes beyond rounding;
+    whatever is changed is not finite."""
+    import torch
+    note(f"linear non-finite {lens} {Hq}/{Hkv} {d} {at} {what} {value}")
+    c = Case(lens, Hq, Hkv, d)
+    i = list(range(len(lens)))
+    want, room = c.oracle(i, i, d ** -0.5)
+    G, h = Hq // Hkv, Hkv - 1
+    head = Hq - 1 if what == "q" else h
+    getattr(c, what)[at, head, 5] = value
+    hit = np.zeros(want[0].shape, bool)
+    heads = slice(head, head + 1) if what == "q" else slice(h * G, (h + 1) * G)
+    hit[at:at + 1 if what == "q" else lens[0], heads, 5 if what == "v" else slice(None)] = True
+    state_hit = np.zeros(want[1].shape, bool)
+    if what == "k":
+        state_hit[0, h, 5, :] = True
+    elif what == "v":
+        state_hit[0, h, :, 5] = True
+    for dt in (torch.float32, torch.bfloat16):
+        state = c.state.clone()
+        got = kp.linear_chunk_attn(c.q, c.k, c.v, state, c.decay, i, i, c.cu, out_dtype=dt)
+        assert not np.isfinite(f64(got)[hit]).any() and not np.isfinite(f64(state)[state_hit]).any()
+        got[torch.from_numpy(hit).cuda()] = torch.from_numpy(want[0][hit]).to(dt).cuda()
+        state[torch.from_numpy(state_hit).cuda()] = torch.from_numpy(want[1][state_hit]).float().cuda()
+        check(got, state, want, room, c, i)
+
+
+def test_an_infinity_in_a_state():
+    """Both calls: the row of the state stays not finite, other heads and sequences are as they would be."""
+    import torch
+    note("linear infinite state")
+    for lens in ([100, 70], [700, 1], [1, 1]):
+        c = Case(lens, 8, 2, 64)
+        i = [0, 1]
+        want, room = c.oracle(i, i, 0.125)
+        c.state[0, 1, 9, 3] = float("inf")
+        calls = [lambda s: kp.linear_chunk_attn(c.q, c.k, c.v, s, c.decay, i, i, c.cu)]
+        if lens == [1, 1]:
+            calls.append(lambda s: kp.linear_decode_attn(c.q, c.k, c.v, s, c.decay, i, i))
+        for call in calls:
+            state = c.state.clone()
+            got = call(state)
+            hit = torch.zeros_like(got, dtype=torch.bool)
+            hit[:lens[0], 4:, 3] = True
+            assert not bool(torch.isfinite(got[hit]).any()) and not bool(torch.isfinite(state[0, 1, 9, 3]))
+            got[hit] = torch.from_numpy(want[0]).float().cuda()[hit]
+            state[0, 1, 9, 3] = float(want[1][0, 1, 9, 3])
+            check(got, state, want, room, c, i)
