@@ -330,7 +330,9 @@ int kv_append_rope(kvp_pool_t pool, int layer, const kvp_rope* rope, const void*
  * Strides are in elements, multiples of 8, and the pointers 16-byte aligned.  head_dim is 64 or 128, num_kv_heads at
  * most KVP_LINEAR_MAX_HEADS, num_q_heads / num_kv_heads 1, 2, 4, 8 or 16.
  * An infinity or NaN in a token's q, k or v leaves earlier tokens, other heads and other sequences as they are; earlier
- * tokens of its head may be rounded another way where it is in v.
+ * tokens of its head may be rounded another way where it is in v.  What they do reach is not finite; linear_decode_attn
+ * keeps infinities as the formulas do, while linear_chunk_attn, whose products take fp32 operands as sums of parts, may
+ * give NaN for an infinity, also for one that a sum beyond the range of bf16 (3.39e38) became.
  * Errors: KVP_ERANGE for a slot outside [-1, num_slots); KVP_EINVAL for a destination that is another sequence's
  * source or destination, or a decay outside (0, 1]; KVP_EUNSUPPORTED for heads or dtypes not named here.
  * ------------------------------------------------------------------------------------------------- */

@@ -62,7 +62,7 @@ __device__ __forceinline__ unsigned pack2(float lo, float hi) {
 __device__ __forceinline__ float low(unsigned w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float high(unsigned w) { return __uint_as_float(w & 0xffff0000u); }
 
-// The bf16 of x and y, packed; x and y become what is left of them.
+// The bf16 of x and y, packed; x and y become what is left of them.  Of an infinity, NaN is left.
 __device__ __forceinline__ unsigned part(float& x, float& y) {
   unsigned w = pack2(x, y);
   asm("" : "+v"(w));  // (or x is converted a second time, alone)

@@ -123,3 +123,18 @@ def test_an_infinity_in_a_state():
             got[hit] = torch.from_numpy(want[0]).float().cuda()[hit]
             state[0, 1, 9, 3] = float(want[1][0, 1, 9, 3])
             check(got, state, want, room, c, i)
+
+
+def test_infinities_of_single_tokens_stay_infinities():
+    """linear_decode_attn computes the formulas as they stand: inf times a positive number is inf, in state and output."""
+    import torch
+    note("linear infinities")
+    q, k, v = (torch.ones(1, 2, 64, dtype=torch.bfloat16, device="cuda") for _ in range(3))
+    state = torch.ones(1, 2, 64, 64, device="cuda")
+    v[0, 1, 7] = float("inf")
+    state[0, 0, 2, 3] = float("-inf")
+    out = kp.linear_decode_attn(q, k, v, state, [0.5, 0.5], [0], [0], scale=1.0)
+    assert bool((state[0, 1, :, 7] == float("inf")).all()) and float(state[0, 0, 2, 3]) == float("-inf")
+    assert float(out[0, 1, 7]) == float("inf") and float(out[0, 0, 3]) == float("-inf")
+    out[0, 1, 7] = out[0, 0, 3] = 96.0
+    assert bool((out == 96.0).all())  # 64 times 0.5 + 1
