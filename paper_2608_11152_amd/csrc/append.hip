@@ -468,7 +468,7 @@ static void launch_append_rope(const AppendRopeArgs& a, hipStream_t s) {
   const int64_t waves = (int64_t)a.kv.n_runs * (a.kv.Hkv + (a.Hq + kFewQueryHeads - 1) / kFewQueryHeads);
   const int q_heads = !whole ? 1 : a.table.interleaved && waves <= kFewWaves ? kFewQueryHeads : kQueryHeads;
   const int q_slots = (a.Hq + q_heads - 1) / q_heads, slots = a.kv.Hkv + q_slots;
-  const int most = (int)((1u << 30) / slots);  // runs of a launch: 31-bit unit indices
+  const int most = std::max(1, ((1 << 26) - 4) / slots);  // runs of a launch, which has fewer than 2^32 threads
   AppendRopeArgs b = a;
   // Rows read streamed: 201 MB of them 86 -> 77 us, 151 MB 57 -> 57, 100 MB 40 -> 44 us.
   const bool stream = a.tokens * (a.Hq + 2 * a.kv.Hkv) * D * 2 >= kStreamBytes;

@@ -1,0 +1,31 @@
+"""kv_append_rope where a call's heads, tokens and positions are at their ends."""
+import numpy as np
+import pytest
+
+from gpu_helpers import note
+from paper_2608_11152_amd import kvpattn as kp
+
+pytestmark = pytest.mark.gpu
+
+
+def test_more_heads_times_tokens_than_one_launch_holds():
+    """65 single tokens of 2^20 query heads, a wave each: more than 2^26 waves, cut into launches."""
+    import torch
+    note("append rope many waves")
+    B, Hq, Hkv, d = 65, 1 << 20, 16, 64
+    g = torch.Generator(device="cuda").manual_seed(8)
+    q = torch.empty(B, Hq, d, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    k, v = (torch.randn(B, Hkv, d, generator=g, device="cuda").to(torch.bfloat16) for _ in range(2))
+    start = np.arange(B, dtype=np.int32) * 3
+    pos = torch.from_numpy(start).cuda()
+    maxp = 13
+    bt = torch.randperm(B * maxp, generator=torch.Generator().manual_seed(9)).to(torch.int32).view(B, maxp).cuda()
+    rope = kp.Rope(10)
+    a, b = (kp.Pool(1, B * maxp, Hkv, d) for _ in range(2))
+    cu = np.arange(B + 1, dtype=np.int32)
+    got = kp.kv_append_rope(a, 0, rope, k, v, bt, start, cu, q=q)
+    kp.kv_append(b, 0, kp.kvp_rope_apply(rope, k, pos), v, bt, start, cu)
+    assert torch.equal(a.layer_raw(), b.layer_raw()) and bool(a.layer_raw().any())
+    want = kp.kvp_rope_apply(rope, q, pos, out=q)
+    assert torch.equal(got, want)
+    a.close(), b.close()
