@@ -301,7 +301,8 @@ int kvp_rope_apply(const kvp_rope* rope, const void* x, int64_t x_token_stride, 
  *           from t * q_stride.  q_out likewise; it may be q with the same stride, or must not overlap it.
  * Strides are in elements, multiples of 8, and the pointers 16-byte aligned; q_out_stride is at least
  * num_q_heads * head_dim, num_q_heads a multiple of num_kv_heads and at most 2^20.  rotary_dim is at most head_dim.  The
- * pool must live on the current device.  Everything else as in kv_append; a token whose page id is outside the pool is skipped, its query is turned all the same. */
+ * pool must live on the current device.  Positions are below 2^31 (KVP_ERANGE).  Everything else as in kv_append; a token
+ * whose page id is outside the pool is skipped, its query is turned all the same. */
 int kv_append_rope(kvp_pool_t pool, int layer, const kvp_rope* rope, const void* k, int64_t k_stride, const void* v,
                    int64_t v_stride, const void* q, int64_t q_stride, void* q_out, int64_t q_out_stride,
                    int num_q_heads, const int32_t* block_tables, int maxp, const int32_t* start_pos,

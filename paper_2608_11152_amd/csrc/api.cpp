@@ -877,6 +877,9 @@ int kv_append_rope(kvp_pool_t pool, int layer, const kvp_rope* rope, const void*
   rc = plan_append(k, v, block_tables, maxp, start_pos, cu_new, num_seqs, gp, &runs);
   if (rc) return rc;
   if (runs.empty()) return KVP_OK;
+  for (int i = 0; i < num_seqs; ++i)
+    if ((int64_t)start_pos[i] + cu_new[i + 1] - cu_new[i] > (1ll << 31))
+      return set_err(KVP_ERANGE, "sequence %d: positions beyond 31 bits", i);
   rc = check_rows(k, k_stride, "k");
   if (!rc) rc = check_rows(v, v_stride, "v");
   if (!rc && q) {

@@ -29,3 +29,25 @@ def test_more_heads_times_tokens_than_one_launch_holds():
     want = kp.kvp_rope_apply(rope, q, pos, out=q)
     assert torch.equal(got, want)
     a.close(), b.close()
+
+
+def test_positions_beyond_31_bits_are_refused():
+    """A row of 2^27 pages and more holds positions that kvp_rope_apply's do not reach; its table is never read."""
+    import torch
+    note("append rope far positions")
+    lib, rope = kp.lib(), kp.Rope(64)
+    pool = kp.Pool(1, 2, 1, 64)
+    x = torch.ones(4, 1, 64, dtype=torch.bfloat16, device="cuda")
+    bt = torch.zeros(1, dtype=torch.int32, device="cuda")
+    cu = np.asarray([0, 4], np.int32)
+
+    def call(start):
+        sp = np.asarray([start], np.int32)
+        return lib.kv_append_rope(pool.handle, 0, rope.ref(), x.data_ptr(), 64, x.data_ptr(), 64, None, 0, None, 0, 0,
+                                  bt.data_ptr(), 1 << 28, sp.ctypes.data, cu.ctypes.data, 1, None, None)
+
+    for start in (2 ** 31 - 1, 2 ** 31 - 3):
+        assert call(start) == kp.KVP_ERANGE
+    torch.cuda.synchronize()
+    assert not bool(pool.layer_raw().any()) and pool.device_error() == kp.KVP_OK
+    pool.close()
