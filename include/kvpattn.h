@@ -286,8 +286,8 @@ int kvp_rope_init(kvp_rope* rope, int rotary_dim, int interleaved, double base, 
  *              heads must not overlap each other.
  *   positions  device int32 [num_tokens], any values
  *   num_heads  at most 2^20;  head_dim  rotary_dim..256
- * Computed in fp32 (the angle modulo a turn in 64-bit integers) and rounded once.  Reads no host memory after it
- * returns, so it can be captured. */
+ * Computed in fp32 (the angle modulo a turn in 64-bit integers, to 2^-32 of a turn) and rounded once.  Reads no host
+ * memory after it returns, so it can be captured. */
 int kvp_rope_apply(const kvp_rope* rope, const void* x, int64_t x_token_stride, int64_t x_head_stride, void* y,
                    int64_t y_token_stride, int64_t y_head_stride, int dtype, const int32_t* positions,
                    int64_t num_tokens, int num_heads, int head_dim, int grad, void* stream);

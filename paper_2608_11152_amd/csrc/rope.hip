@@ -46,7 +46,7 @@ __global__ __launch_bounds__(256) void rope_pair_kernel(RopeArgs a) {
 
 // A head in units of 8 dims, 16 bytes of bf16 a load: in the half layout a unit and the one R / 2 further, in the
 // interleaved one a unit alone; dims that are not rotated follow.  A thread holds one unit of up to N heads of a token,
-// whose sines and cosines (35 instructions a pair) it computes once, while the loads are under way.  16384 tokens of 36
+// whose sines and cosines (32 instructions a pair) it computes once, while the loads are under way.  16384 tokens of 36
 // heads of 128, bf16 (302 MB): 55 us, 5.5 TB/s where a copy reaches 5.1; 5003 tokens of 32 heads, fp32, half of each head
 // rotated (164 MB): 31 us, 5.2 TB/s.
 template <class T, bool IL, int N, bool Stream>

@@ -2,7 +2,8 @@
 //
 // Pair i of a token at position p is turned by p * f_i radians.  The host passes f_i as the fraction of a turn per
 // position, 2^64 f_i / (2 pi) rounded to an integer (kvp_rope.turns), so the product with p modulo 2^64 is the angle
-// modulo one turn with no loss at far positions: the table's half step times 2^31 positions is 2^-34 of a turn.
+// modulo one turn with hardly a loss at far positions: the table's half step times 2^31 positions is 2^-34 of a turn.  The
+// sine takes the angle rounded to 2^-32 of a turn, at any position.
 #pragma once
 #include <hip/hip_runtime.h>
 
@@ -12,11 +13,12 @@
 
 namespace kvp {
 
-// sin and cos of phase / 2^64 turns.  The nearest quarter turn is taken out in integers; what remains, |x| <= pi / 4,
-// goes into the Taylor series (first terms left out: x^11 / 11! = 2e-9, x^12 / 12! = 1e-10, under half a step of fp32).
+// sin and cos of phase / 2^64 turns.  The phase is rounded to 2^-32 of a turn, 2^-33 (7.3e-10 radian) off at most.  The
+// nearest quarter turn is taken out in integers; what remains, |x| <= pi / 4, goes into the Taylor series (first terms left
+// out: x^11 / 11! = 2e-9, x^12 / 12! = 1e-10, under half a step of fp32).
 __device__ __forceinline__ void sincos_turns(uint64_t phase, float* sn, float* cs) {
-  const unsigned quad = (unsigned)((phase + (1ull << 61)) >> 62);
-  const int r = (int)((int64_t)(phase - ((uint64_t)quad << 62)) >> 32);
+  const unsigned top = (unsigned)((phase + (1ull << 31)) >> 32), quad = (top + (1u << 29)) >> 30;
+  const int r = (int)(top - (quad << 30));
   const float x = (float)r * 1.4629180792671596e-9f;  // 2 pi / 2^32
   const float y = x * x;
   const float s = fmaf(x * y, fmaf(y, fmaf(y, fmaf(y, 1.0f / 362880.0f, -1.0f / 5040.0f), 1.0f / 120.0f), -1.0f / 6.0f), x);
