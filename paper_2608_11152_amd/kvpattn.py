@@ -7,6 +7,7 @@ The names follow the C-ABI in include/kvpattn.h.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import math
 import os
 
@@ -382,24 +383,53 @@ class Rope:
         return self._ref
 
 
+@functools.lru_cache(maxsize=None)
+def _rope_function():
+    """kvp_rope_apply as autograd knows it: the gradient of a turn is the turn back.  (torch is imported by the calls.)"""
+    import torch
+
+    class RopeApply(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, rope, positions, grad, stream):
+            ctx.save_for_backward(positions)
+            ctx.rope, ctx.grad = rope, grad
+            return kvp_rope_apply(rope, x, positions, grad=grad, stream=stream)
+
+        @staticmethod
+        def backward(ctx, g):  # on the current stream, as all of autograd's work
+            positions, = ctx.saved_tensors
+            g = g if g.stride(2) == 1 else g.contiguous()
+            return kvp_rope_apply(ctx.rope, g, positions, grad=not ctx.grad), None, None, None, None
+
+    return RopeApply
+
+
 def kvp_rope_apply(rope: Rope, x, positions, out=None, grad: bool = False, stream=None):
     """The heads of x [T, H, d] (bf16 or fp32, tokens and heads at any stride) turned by positions (device int32 [T]);
-    grad: the transpose, for the gradient.  `out` may be x; a new tensor is dense."""
+    grad: the transpose, for the gradient.  `out` may be x; a new tensor is dense.  Autograd records the call; one with
+    `out` it cannot, so that is refused where a gradient is asked for."""
     import torch
     dtypes = (torch.bfloat16, torch.float32)
     (T, H, d), xs = _heads(x, "x", dtypes)
     _dev(positions, "positions", _i32t(), 1, rows=T)
     if positions.get_device() != x.get_device():
         raise ValueError(f"positions is on {positions.device}, x on {x.device}")
-    if out is None:
-        out, ys = _alloc_on(stream, (T, H, d), x.dtype, x.device), (H * d, d)
-    else:
+    given = out is not None
+    if given:
         shape, ys = _heads(out, "out", (x.dtype,))
         if shape != x.shape:
             raise ValueError(f"out has shape {tuple(shape)}, x {tuple(x.shape)}")
+        if (x.requires_grad or out.requires_grad) and torch.is_grad_enabled():
+            raise ValueError("out takes no part in autograd: leave it away, or call under torch.no_grad()")
+    elif x.requires_grad and torch.is_grad_enabled():
+        return _rope_function().apply(x, rope, positions, bool(grad), stream)
+    else:
+        out, ys = _alloc_on(stream, (T, H, d), x.dtype, x.device), (H * d, d)
     _check(lib().kvp_rope_apply(rope.ref(), x.data_ptr(), xs[0], xs[1], out.data_ptr(), ys[0], ys[1],
                                 KVP_F32 if x.dtype == torch.float32 else KVP_BF16, positions.data_ptr(), T, H, d, int(grad),
                                 _stream(stream)), "kvp_rope_apply")
+    if given:  # autograd must not use what it had saved of it
+        torch.autograd.graph.increment_version(out)
     return out
 
 

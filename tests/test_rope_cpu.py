@@ -114,3 +114,11 @@ def test_oracle_gradient_is_the_derivative(interleaved):
         e[i] = 1.0
         want[i] = ((rotary.rotate(x + e, pos, f, interleaved, 1.2) - rotary.rotate(x - e, pos, f, interleaved, 1.2)) * g).sum() / 2
     assert np.allclose(rotary.rotate(g, pos, f, interleaved, 1.2, grad=True), want)
+
+
+def test_binding_refuses_what_is_no_gpu_tensor_whether_it_has_a_gradient_or_not():
+    import torch
+    pos = torch.zeros(4, dtype=torch.int32)
+    for x in (np.zeros((4, 8, 64), np.float32), torch.zeros(4, 8, 64, requires_grad=True)):
+        with pytest.raises(ValueError, match="GPU tensor"):
+            kp.kvp_rope_apply(kp.Rope(64), x, pos)
