@@ -298,7 +298,8 @@ int kvp_rope_apply(const kvp_rope* rope, const void* x, int64_t x_token_stride, 
  *   k, v    device bf16: token t's num_kv_heads * head_dim elements from t * k_stride, t * v_stride (rows of a fused
  *           projection, for instance)
  *   q       device bf16, nullable (then q_out and num_q_heads are ignored): token t's num_q_heads * head_dim elements
- *           from t * q_stride.  q_out likewise; it may be q with the same stride, or must not overlap it.
+ *           from t * q_stride.  q_out likewise; it may be q with the same stride, or must not overlap it.  Its rows
+ *           from cu_new[num_seqs] on are left as they were.
  * Strides are in elements, multiples of 8, and the pointers 16-byte aligned; q_out_stride is at least
  * num_q_heads * head_dim, num_q_heads a multiple of num_kv_heads and at most 2^20.  rotary_dim is at most head_dim.  The
  * pool must live on the current device.  Positions are below 2^31 (KVP_ERANGE).  Everything else as in kv_append; a token
@@ -344,7 +345,7 @@ int kv_append_rope(kvp_pool_t pool, int layer, const kvp_rope* rope, const void*
 int linear_chunk_workspace_size(const int32_t* cu, int num_seqs, int num_kv_heads, int head_dim, size_t* bytes);
 
 /* Chunks: sequence i's tokens are the rows cu[i] .. cu[i+1] (none: its state is handed on as it is).
- *   cu  host int32 [num_seqs + 1], non-decreasing, cu[0] = 0
+ *   cu  host int32 [num_seqs + 1], non-decreasing, cu[0] = 0; rows of out from cu[num_seqs] on are left as they were
  *   ws  device workspace of ws_bytes >= linear_chunk_workspace_size(...), 16-byte aligned
  * The strides are head_dim .. 2^24.  Errors: KVP_EWORKSPACE if ws is too small. */
 int linear_chunk_attn(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,

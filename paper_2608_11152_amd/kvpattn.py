@@ -436,7 +436,8 @@ def kvp_rope_apply(rope: Rope, x, positions, out=None, grad: bool = False, strea
 def kv_append_rope(pool: Pool, layer, rope: Rope, k, v, block_tables, start_pos, cu_new, q=None, q_out=None,
                    group_prefix=None, stream=None):
     """kv_append with the keys turned to their positions, and with q [T, Hq, d] the same tokens' queries, returned (in
-    `q_out`, which may be q).  k, v, q: device bf16, tokens at any stride that is a multiple of 8 elements."""
+    `q_out`, which may be q).  k, v, q: device bf16, tokens at any stride that is a multiple of 8 elements.  Rows of the
+    output behind the last sequence are not written: what a new tensor holds there is undefined."""
     sp, cu = _i32(start_pos), _i32(cu_new)
     if len(cu) != len(sp) + 1:
         raise ValueError(f"cu_new has {len(cu)} entries, {len(sp) + 1} needed")
@@ -500,7 +501,9 @@ def linear_chunk_workspace_size(cu, num_kv_heads: int, head_dim: int) -> int:
 def linear_chunk_attn(q, k, v, state, decay, src_slots, dst_slots, cu, scale=None, out=None, out_dtype=None, ws=None,
                       stream=None):
     """Linear attention of ragged chunks: q [T, Hq, d], k, v [T, Hkv, d] device bf16 (tokens at any stride that is a
-    multiple of 8 elements), state device fp32 [slots, Hkv, d, d]; decay, src_slots, dst_slots, cu host."""
+    multiple of 8 elements), state device fp32 [slots, Hkv, d, d]; decay, src_slots, dst_slots, cu host.  Returns fp32
+    unless out_dtype (or out) is bf16, which is quicker.  Rows of the output behind the last sequence are not written:
+    what a new tensor holds there is undefined."""
     import torch
     cu = _i32(cu)
     if len(cu) != len(src_slots) + 1:
