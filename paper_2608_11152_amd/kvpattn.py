@@ -455,6 +455,8 @@ def kv_append_rope(pool: Pool, layer, rope: Rope, k, v, block_tables, start_pos,
             os_ = _rows(q_out, "q_out", T, Hq, pool.head_dim)
     elif q_out is not None:
         raise ValueError("q_out without q")
+    if block_tables.get_device() != k.get_device():
+        raise ValueError(f"block_tables is on {block_tables.device}, k on {k.device}")
     _check(lib().kv_append_rope(pool.handle, layer, rope.ref(), k.data_ptr(), ks, v.data_ptr(), vs,
                                 None if q is None else q.data_ptr(), qs, None if q is None else q_out.data_ptr(), os_, Hq,
                                 block_tables.data_ptr(), block_tables.shape[1], _addr(sp), _addr(cu), len(sp),
@@ -519,6 +521,8 @@ def linear_chunk_attn(q, k, v, state, decay, src_slots, dst_slots, cu, scale=Non
         ws = _alloc_on(stream, linear_chunk_workspace_size(cu, k.shape[1], k.shape[2]), torch.uint8, q.device)
     else:
         _dev(ws, "ws", (ws.dtype,))
+        if ws.get_device() != q.get_device():
+            raise ValueError(f"ws is on {ws.device}, q on {q.device}")
     _check(lib().linear_chunk_attn(*head, addr, *tail, ws.data_ptr(), ws.numel() * ws.element_size(), s),
            "linear_chunk_attn")
     return out

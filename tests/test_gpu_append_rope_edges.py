@@ -51,3 +51,42 @@ def test_positions_beyond_31_bits_are_refused():
     torch.cuda.synchronize()
     assert not bool(pool.layer_raw().any()) and pool.device_error() == kp.KVP_OK
     pool.close()
+
+
+class Elsewhere:
+    """A tensor that says it is on the second device."""
+
+    def __init__(self, t):
+        self.t, self.is_cuda, self.device = t, True, "cuda:1"
+
+    def get_device(self):
+        return 1
+
+    def __getattr__(self, name):
+        return getattr(self.t, name)
+
+
+def test_tensors_of_another_device_are_refused():
+    import torch
+    note("append rope another device")
+    rope, pool = kp.Rope(64), kp.Pool(1, 4, 2, 64)
+    x = torch.ones(3, 2, 64, dtype=torch.bfloat16, device="cuda")
+    bt = torch.zeros(1, 1, dtype=torch.int32, device="cuda")
+    pos = torch.zeros(3, dtype=torch.int32, device="cuda")
+    state = torch.zeros(1, 2, 64, 64, device="cuda")
+    ws = torch.zeros(1 << 20, dtype=torch.uint8, device="cuda")
+    far = Elsewhere
+    calls = [lambda: kp.kv_append_rope(pool, 0, rope, x, x, far(bt), [0], [0, 3]),
+             lambda: kp.kv_append_rope(pool, 0, rope, far(x), x, bt, [0], [0, 3]),
+             lambda: kp.kv_append_rope(pool, 0, rope, x, x, bt, [0], [0, 3], q=x, q_out=far(x)),
+             lambda: kp.kvp_rope_apply(rope, x, far(pos)),
+             lambda: kp.kvp_rope_apply(rope, x, pos, out=far(x)),
+             lambda: kp.linear_chunk_attn(x, x, x, state, [1.0, 1.0], [0], [0], [0, 3], ws=far(ws)),
+             lambda: kp.linear_chunk_attn(x, x, x, far(state), [1.0, 1.0], [0], [0], [0, 3]),
+             lambda: kp.linear_decode_attn(x[:1], x[:1], far(x[:1]), state, [1.0, 1.0], [0], [0])]
+    for call in calls:
+        with pytest.raises(ValueError, match="device|is on"):
+            call()
+    torch.cuda.synchronize()
+    assert not bool(pool.layer_raw().any()) and not bool(state.any())
+    pool.close()
