@@ -272,7 +272,8 @@ typedef struct kvp_rope {
  *   factor        >= 1: contexts are factor times longer than the original ones (1: as they are)
  *   original_len  0: every f_i is divided by factor.  > 0: with n_i = original_len f_i / (2 pi) turns over the original
  *                 context and g_i = (n_i - low_turns) / (high_turns - low_turns) clamped to [0, 1],
- *                 f_i becomes (1 - g_i) f_i / factor + g_i f_i  (0 <= low_turns < high_turns)
+ *                 f_i becomes (1 - g_i) f_i / factor + g_i f_i  (0 <= low_turns < high_turns).  (A ramp over the pair
+ *                 index between two rounded indices, which some programs use, gives other frequencies; it is not offered.)
  *   magnitude     the rotated dims are multiplied by it (1: none; finite, > 0)
  * Pure host computation.  Errors: KVP_EINVAL for a value outside these ranges. */
 int kvp_rope_init(kvp_rope* rope, int rotary_dim, int interleaved, double base, double factor, int original_len,

@@ -256,8 +256,10 @@ __global__ __launch_bounds__(256) void gather_kernel(GatherArgs a) {
 // R / 2 further or the next ones that are not rotated), computes its sines and cosines once and uses them for all of the
 // wave's heads; a run of few tokens spreads the heads over the lanes.  Bandwidth is what bounds it: 16416 tokens of 32 + 4
 // heads of 128 (336 MB) take 64 us, 5.3 TB/s where a copy reaches 5.1; 3567 tokens into FP8 pages 15.4 us, 4.5 TB/s.
-// A step of 512 single tokens (11 us) waits for its run records, which lie in pinned host memory, then for page ids, then
-// for rows.
+// A step of 512 single tokens (11 us for 10.5 MB) is a chain of waits: a key wave's for its run record in pinned host memory
+// (in two trips), the page id, the row of v, the row of k, the rotation's table, then put_v's D / 32 rounds of pieces, which
+// are read, changed and written one round after the other (with one token in the page 2 bytes of each 16: 9.7 MB read and 9.4
+// written in all).
 //
 // Query heads of a wave: 8, or 4 in the interleaved layout (whose waves take twice the passes over a run) where the waves
 // of a call have room beside each other.  4160 tokens with 8 / 4: 32 + 2 heads interleaved 18.1 / 17.0 us, 8 + 8 17.0 /

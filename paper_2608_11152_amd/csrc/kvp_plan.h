@@ -1,4 +1,4 @@
-// Host-side planning for the paged attention kernels: validation of host metadata and the split-KV /
+// Host-side planning for the paged attention kernels and linear attention: validation of host metadata and the split-KV /
 // shared-prefix work lists the kernels consume.  Pure C++ (no HIP), so it builds and tests on a CPU.
 #pragma once
 #include <cstdint>

@@ -27,15 +27,15 @@
 // neighbour.  One part for S and P would take 6% less time, with 2^-9 of the state in every output.
 //
 // Three workgroups fit a compute unit (50 KB of LDS; 149 VGPRs, which the sched_barriers and Lane keep them at).  64
-// prompts of 128 .. 1024 tokens with 16 heads of 128, 663 MB: 161 us, 4.1 TB/s of the 5.1 that a copy reaches.  The SIMDs
-// bound it: matrix instructions take 35% and vector instructions 41% of the cycles at 2.1 GHz, and add up; without the
-// former it takes 135 us.
+// prompts of 128 .. 1024 tokens with 16 heads of 128, 663 MB: 158 us, 4.2 TB/s of the 5.1 that a copy reaches.  A SIMD has
+// a matrix instruction under way in 35% of the cycles, a vector instruction in 42%, either in 66%; its waves wait for loads,
+// LDS and barriers 29% of their time and for their turn to issue 39%.
 //
 // A sequence that would leave compute units without work is cut into parts (plan_linear): linear_sum_kernel sums each part
 // from zeros, linear_scan_kernel turns the sums into the states before the parts, and the parts are items.  The parts'
-// keys and values are read twice: 131071 tokens with 16 heads of 128 take 770 us, 216 of them the sums (206 GFLOP: V
-// in 3 parts), 19 the scan, 496 the chunks (2.1 GB, 4.3 TB/s).  Under a load this long the clock is 1.7 GHz and the SIMDs are
-// busy 90% of it: with every tile from the caches the sums take 190 us and the chunks 443, without outputs too 403.
+// keys and values are read twice: 131071 tokens with 16 heads of 128 take 765 us, 225 of them the sums (1.1 GB, 4.9 TB/s;
+// 206 GFLOP: V in 3 parts), 18 the scan, 514 the chunks (2.2 GB, 4.3 TB/s; the SIMDs have an instruction under way in 73% of
+// the cycles).
 #include <algorithm>
 
 #include "rope_dev.h"

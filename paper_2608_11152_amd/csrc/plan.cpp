@@ -1,4 +1,4 @@
-// Host planner: validates host metadata and builds the work lists of the decode and prefill kernels.
+// Host planner: validates host metadata and builds the work lists of the decode, prefill and linear attention kernels.
 // Deterministic: a plan depends only on lengths, group structure, head counts and the pool's element
 // type, never on physical page ids, so GPU results are bitwise reproducible under any page permutation.
 #include <algorithm>
