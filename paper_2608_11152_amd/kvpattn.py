@@ -2,7 +2,8 @@
 path runs in the HIP library; there is no fallback.  Device arrays are torch tensors on the GPU (torch
 provides device memory and streams), host metadata arrays are numpy int32.
 
-The names follow the C-ABI in include/kvpattn.h.
+The names follow the C-ABI in include/kvpattn.h.  Of all calls, kvp_rope_apply alone is recorded by autograd; what
+the others return is detached.
 """
 from __future__ import annotations
 
